@@ -515,6 +515,218 @@ janus_status janus_loss_reduce(janus_loss_kind kind, const float* h, int64_t n,
                                float* loss, float* dh, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Short causal convolution                                                 */
+/* ------------------------------------------------------------------------ */
+/*
+ * A depthwise convolution over the last K inputs of each channel, the local
+ * mixing that goes before a selective scan:
+ *     p_t[d] = bias[d] + sum_k w[d, k] x_{t-K+1+k}[d],   y = p  or  p s(p)
+ * over variable-length sequences as in janus_lstm_seq_fwd: sequence b runs
+ * while t < lengths[b], its inputs before t = 0 are its carried state, and
+ * its output is 0 from lengths[b] on (x is not read there).
+ */
+typedef enum { JANUS_CONV_LINEAR = 0, JANUS_CONV_SILU = 1 } janus_conv_act;
+
+/* D channels, K taps (1 to 8), batch B, T time steps.  Row (t, b) of x and dx
+ * starts ldx elements after the row before it, of y and dy ldy (0: dense, D;
+ * else at least D), so x may be a column slice of a wider matrix. */
+typedef struct {
+    int32_t D, K, B, T;
+    janus_dtype dtype;
+    janus_conv_act act;
+    int64_t ldx, ldy;
+} janus_conv_desc;
+
+/* Bytes of workspace of janus_causal_conv_bwd (0 for a bad descriptor). */
+size_t janus_causal_conv_workspace_bytes(const janus_conv_desc* d);
+
+/*
+ *  x        [T, B, D] dtype, row stride ldx.
+ *  lengths  host int32 [B] with 0 <= len <= T, or NULL for all T.
+ *  w        [D, K] dtype, the last tap on the present input; bias [D] dtype
+ *           or NULL (zero).
+ *  s0       [B, K-1, D] dtype, the inputs before t = 0, oldest first, or NULL
+ *           (zeros).
+ *  y        [T, B, D] dtype, row stride ldy; not x.
+ *  sT       [B, K-1, D] dtype or NULL: the last K - 1 inputs of each sequence
+ *           (of s0 where it is shorter); not s0.
+ * Errors: NULL d/w, NULL x or y with T > 0, a non-positive D, K, B, T < 0, a
+ * stride below D, a pointer not aligned to its element, y = x, or sT = s0 ->
+ * INVALID_ARG; K > 8, a dtype or act not listed -> UNSUPPORTED; a length
+ * outside [0, T] -> LENGTH.
+ */
+janus_status janus_causal_conv_fwd(const janus_conv_desc* d, const void* x, const int32_t* lengths,
+                                   const void* w, const void* bias, const void* s0, void* y, void* sT,
+                                   void* stream);
+
+/*
+ * Backward of the call above (same d, x, lengths, w, bias, s0; nothing kept).
+ *  dy       [T, B, D] dtype, row stride ldy; not read from lengths[b] on.
+ *  dsT      [B, K-1, D] float32 gradient of sT, or NULL (zero).
+ *  dx       [T, B, D] dtype, row stride ldx, or NULL; 0 from lengths[b] on;
+ *           not x or dy.
+ *  dw [D, K], dbias [D]: float32, either may be NULL.
+ *  ds0      [B, K-1, D] float32 or NULL.
+ * The sums over time and batch are taken in a fixed order.
+ * Errors: as the forward; NULL dy with T > 0 -> INVALID_ARG; WORKSPACE.
+ */
+janus_status janus_causal_conv_bwd(const janus_conv_desc* d, const void* x, const int32_t* lengths,
+                                   const void* w, const void* bias, const void* s0, const void* dy,
+                                   const float* dsT, void* dx, float* dw, float* dbias, float* ds0,
+                                   void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One step of B running sequences (d->T is not used): row b takes its input
+ * x[b] (row stride ldx), writes y[b] (row stride ldy) and moves its state on.
+ *  slots    device int32 [B] or NULL (row b has slot b): the slot of each
+ *           row's sequence in `state`.  A slot outside [0, n_slots) marks a
+ *           row that does not run: its y is 0 and no state changes.  Running
+ *           rows have slots of their own.
+ *  state    [n_slots, K-1, D] dtype, updated in place (sT of a prompt is
+ *           such a state).  May be NULL when K is 1.
+ * Errors: as the forward; n_slots < 1 (or < B with slots NULL) -> INVALID_ARG.
+ */
+janus_status janus_causal_conv_step(const janus_conv_desc* d, const void* x, const void* w, const void* bias,
+                                    const int32_t* slots, int32_t n_slots, void* state, void* y, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Selective scan                                                           */
+/* ------------------------------------------------------------------------ */
+/*
+ * A recurrence of N states per channel without a hidden-to-hidden product,
+ * whose decay and input weights come from the data (the loop of Figure 1 with
+ * a cell of its own):
+ *     v = dt_t[d] + dt_bias[d],   e = log(1 + exp(v)) with SOFTPLUS, else v
+ *     h_t[d, n] = exp(e A[d, n]) h_{t-1}[d, n] + e B_t[g, n] x_t[d]
+ *     y_t[d] = (sum_n C_t[g, n] h_t[d, n] + Dskip[d] x_t[d]) * (z_t[d] s(z_t[d]))
+ * with g = d / (D / G), the last factor only with a gate z.  Sequence b runs
+ * while t < lengths[b]; its state is then carried unchanged and its y is 0
+ * (nothing of its later rows is read).
+ */
+#define JANUS_SCAN_SOFTPLUS 1   /* e = log(1 + exp(v)) */
+#define JANUS_SCAN_KEEP 2       /* the forward keeps in the workspace what its backward needs */
+
+/* D channels in G groups (D a multiple of G), N states per channel (1 to 64),
+ * batch B, T time steps.  The ld* are the row strides, in elements, of x (and
+ * dx), dt (ddt), Bm (dBm), Cm (dCm), z (dz) and y (dy); 0: dense rows (D, or
+ * G N for Bm and Cm); else at least that. */
+typedef struct {
+    int32_t D, N, G, B, T;
+    janus_dtype dtype;
+    int32_t flags;
+    int64_t ldx, ldt, ldb, ldc, ldz, ldy;
+} janus_scan_desc;
+
+/* Bytes of workspace of janus_selective_scan_fwd / _bwd (0 for a bad
+ * descriptor; may be 0 without KEEP). */
+size_t janus_selective_scan_workspace_bytes(const janus_scan_desc* d);
+
+/*
+ *  x, dt    [T, B, D] dtype;  Bm, Cm [T, B, G, N] dtype;  z [T, B, D] dtype
+ *           or NULL (no gate).
+ *  lengths  host int32 [B] with 0 <= len <= T, or NULL for all T.
+ *  A        [D, N] float32 (the exponent e A is a product that spans orders
+ *           of magnitude; 16 bits would move the slow decays);  Dskip,
+ *           dt_bias [D] float32 or NULL (zero).
+ *  h0, hT   [B, D, N] float32 or NULL (zeros; not wanted); hT may be h0.
+ *  y        [T, B, D] dtype; not an input.
+ * Errors: NULL d/A, NULL x/dt/Bm/Cm/y with T > 0, a non-positive D, N, G, B,
+ * T < 0, D not a multiple of G, a stride below a row, a pointer not aligned to
+ * its element -> INVALID_ARG; N > 64, a dtype or flag not listed ->
+ * UNSUPPORTED; LENGTH; WORKSPACE.
+ */
+janus_status janus_selective_scan_fwd(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
+                                      const void* Bm, const void* Cm, const float* Dskip, const void* z,
+                                      const float* dt_bias, const int32_t* lengths, const float* h0,
+                                      void* y, float* hT, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward of the call above, made with KEEP (same arguments and workspace; h0
+ * unchanged).
+ *  dy       [T, B, D] dtype, row stride ldy; not read from lengths[b] on.
+ *  dhT      [B, D, N] float32 gradient of hT, or NULL (zero).
+ *  dx, ddt, dz [T, B, D], dBm, dCm [T, B, G, N] dtype, with the row strides of
+ *           x, dt, z, Bm, Cm; 0 from lengths[b] on.  dz may be NULL without z.
+ *  dA [D, N], dDskip, ddt_bias [D], dh0 [B, D, N]: float32; the last three
+ *           may be NULL.  The sums are taken in a fixed order.
+ * Errors: as the forward; NULL dy/dx/ddt/dBm/dCm with T > 0, NULL dA, NULL dz
+ * with z, or a descriptor without KEEP -> INVALID_ARG.
+ */
+janus_status janus_selective_scan_bwd(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
+                                      const void* Bm, const void* Cm, const float* Dskip, const void* z,
+                                      const float* dt_bias, const int32_t* lengths, const float* h0,
+                                      const void* dy, const float* dhT, void* dx, void* ddt, float* dA,
+                                      void* dBm, void* dCm, float* dDskip, void* dz, float* ddt_bias,
+                                      float* dh0, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One step of B running sequences (d->T is not used): one row of each input
+ * per sequence, with the row strides of d.
+ *  slots, n_slots  as janus_causal_conv_step.
+ *  state    [n_slots, D, N] float32, updated in place (hT of a prompt is such
+ *           a state).
+ * Errors: as the forward; n_slots < 1 (or < B with slots NULL) -> INVALID_ARG.
+ */
+janus_status janus_selective_scan_step(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
+                                       const void* Bm, const void* Cm, const float* Dskip, const void* z,
+                                       const float* dt_bias, const int32_t* slots, int32_t n_slots,
+                                       float* state, void* y, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Clipped policy loss                                                      */
+/* ------------------------------------------------------------------------ */
+/*
+ * The loss of a policy step over sampled actions (tokens), from the logits of
+ * each row.  With l = x[a] - log sum exp(x), the log-probability of the row's
+ * action, r = exp(l - old), H the entropy of softmax(x) and u = ref - l:
+ *     row  = -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv)
+ *            + kl_coef (exp(u) - 1 - u) - ent_coef H
+ *     loss = sum w row / sum w
+ * and the gradient of the logits.  The gradient of the first term is that of
+ * -r adv where r adv is the smaller of the two or equal to the other, else 0.
+ * A row of weight 0 or with a negative action (padding) does not count: its
+ * gradient is 0 whatever its values are, and it adds nothing to any sum.
+ * Logits of -inf (forbidden actions) have probability 0; a row with nothing
+ * but -inf has l = -inf, H = 0, adds 0 to the sums and has gradient 0.  A row
+ * that counts and whose action is V or more, or whose logits hold a NaN or
+ * +inf, makes its outputs and the loss NaN (janus_sgd_clip_update then leaves
+ * the parameters as they are).  When no row counts, loss and gradient are 0.
+ */
+typedef struct {
+    int32_t rows, V;
+    janus_dtype dtype;
+    int64_t ld;             /* elements between rows of logits and dlogits; 0: V */
+    float clip_low, clip_high, kl_coef, ent_coef;   /* finite; the clips not negative */
+} janus_policy_desc;
+
+/* Bytes of workspace of janus_policy_loss (0 for a bad descriptor). */
+size_t janus_policy_workspace_bytes(const janus_policy_desc* d);
+
+/*
+ *  logits   [rows, V] dtype, row stride ld.
+ *  actions  device int32 [rows]; checked on the device (above), since actions
+ *           are sampled there.
+ *  old_logp, adv [rows] float32; ref_logp [rows] float32 or NULL (no KL term);
+ *           weights [rows] float32, finite and not negative, or NULL (ones).
+ *  dlogits  [rows, V] dtype, row stride ld; may be logits itself.
+ *  logp, entropy [rows] float32, each may be NULL: l and H of every row (0
+ *           for a negative action), also of rows of weight 0.
+ *  stats    float32 [6] or NULL: loss, and the weighted means of its first
+ *           term, of the KL estimate (0 without ref_logp), of H and of the
+ *           share of rows whose gradient the clip cut off; the sum of weights.
+ * Scoring: with dlogits, old_logp and adv NULL only logp and entropy are
+ * formed (stats must be NULL; weights, ref_logp and ws are not used).
+ * Errors: NULL d/logits/actions, dlogits without old_logp or adv or the
+ * reverse, stats when scoring, a non-positive size, ld below V, a bad
+ * coefficient, a pointer not aligned to its element -> INVALID_ARG; dtype not
+ * F32/BF16 -> UNSUPPORTED; WORKSPACE.
+ */
+janus_status janus_policy_loss(const janus_policy_desc* d, const void* logits, const int32_t* actions,
+                               const float* old_logp, const float* adv, const float* ref_logp,
+                               const float* weights, void* dlogits, float* logp, float* entropy, float* stats,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Tracing                                                                  */
 /* ------------------------------------------------------------------------ */
 

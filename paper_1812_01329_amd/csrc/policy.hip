@@ -1,0 +1,423 @@
+// Clipped policy loss from logits: rows' log-probabilities and entropies, the
+// loss with its KL and entropy terms, and the gradient of the logits.
+//
+//   M = max x,  S = sum exp(x - M),  E = sum exp(x - M)(x - M)
+//   l = x[a] - M - log S,   H = log S - E / S,   p_j = exp(x_j - M) / S
+//   row  = -min(r adv, clip(r) adv) + beta (exp(u) - 1 - u) - eta H,   r = exp(l - old), u = ref - l
+//   c    = d row / d l = -r adv [r adv <= clip(r) adv] - beta (exp(u) - 1)
+//   dx_j = w / W (c (1[j = a] - p_j) + eta p_j (log p_j + H)),   W = sum w
+//
+// One workgroup a row, which it holds in registers between the sums and the
+// gradient, so the logits are read once and the gradient written once; rows
+// past 64K float32 or 128K bf16 are read twice.  Sums are float32 (float64 over
+// the rows) in a fixed order.
+#include <cmath>
+
+#include "seq.hpp"
+
+namespace janus {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFarBelow = -200.f;   // exp is 0 there: keeps 0 * -inf out of the sums
+
+struct PolicyArgs {
+    int32_t rows, V;
+    int64_t ld;
+    const void* logits;
+    const int32_t* actions;
+    const float *old_logp, *adv, *ref, *weights;
+    void* dlogits;        // NULL: scoring
+    float *logp, *entropy;
+    const float* W;       // sum of the weights that count
+    float4* terms;        // [rows] weighted first term, KL, H, clipped
+    float lo, hi, beta, eta;
+};
+
+__device__ __forceinline__ float wsum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ __forceinline__ float wmax(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+__device__ __forceinline__ double wsum(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+__device__ __forceinline__ float exp_(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+
+// A product that stays rounded: contracted into the sum it goes into, c w / W
+// would leave its rounding error where the gradient is 0 (p = 1 at the action)
+__device__ __forceinline__ float rounded_mul(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+// exp(u) - 1 - u without the cancellation near 0
+__device__ __forceinline__ float kl_term(float u) {
+    if (fabsf(u) < 0.5f)
+        return u * u *
+               (0.5f + u * (1.f / 6 + u * (1.f / 24 + u * (1.f / 120 + u * (1.f / 720 + u * (1.f / 5040 + u / 40320))))));
+    return expm1f(u) - u;
+}
+
+template <typename T>
+struct Piece {   // 16 bytes of a row
+    static constexpr int VEC = 16 / sizeof(T);
+    uint4 v;
+    __device__ __forceinline__ float get(int j) const {
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(&v);
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u[j]);
+        else return j & 1 ? hi2f(u[j / 2]) : lo2f(u[j / 2]);
+    }
+    __device__ __forceinline__ void set(int j, T x) {
+        T t[VEC];
+        __builtin_memcpy(t, &v, 16);
+        t[j] = x;
+        __builtin_memcpy(&v, t, 16);
+    }
+};
+
+// Rows start at any element; a row is cut at 16-byte boundaries of memory, so
+// only its first and last piece can be partial: those go element by element, and
+// elements outside the row count as -inf.
+template <typename T>
+struct Row {
+    static constexpr int VEC = 16 / sizeof(T);
+    const T* base;   // first element's 16-byte boundary (not all of the first piece is the row's)
+    int lo, hi;      // the row: elements [lo, hi) from base
+    __device__ __forceinline__ Row(const T* p, int V) {
+        const int mis = int(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(T));
+        base = p - mis, lo = mis, hi = mis + V;
+    }
+    __device__ __forceinline__ int pieces() const { return (hi + VEC - 1) / VEC; }
+    __device__ __forceinline__ bool whole(int p) const { return p * VEC >= lo && p * VEC + VEC <= hi; }
+    __device__ __forceinline__ Piece<T> load(int p) const {
+        Piece<T> r;
+        if (whole(p)) {
+            r.v = *reinterpret_cast<const uint4*>(base + int64_t(p) * VEC);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int i = p * VEC + j;
+                r.set(j, i >= lo && i < hi ? base[i] : from_f<T>(-INFINITY));
+            }
+        }
+        return r;
+    }
+    // to another row with the same cut (or `same` false: element by element)
+    __device__ __forceinline__ void store(T* out, bool same, int p, const float* f) const {
+        if (same && whole(p)) {
+            Chan<T, VEC>::store(out + int64_t(p) * VEC, f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int i = p * VEC + j;
+                if (i >= lo && i < hi) out[i] = from_f<T>(f[j]);
+            }
+        }
+    }
+};
+
+// M, S, E of values seen so far; values join by pieces
+struct Soft {
+    float m = -INFINITY, s = 0.f, e = 0.f;
+    __device__ __forceinline__ void add(float t) {   // t = x - m
+        const float v = exp_(t);
+        s += v;
+        e = fmaf(v, fmaxf(t, kFarBelow), e);
+    }
+    // to a maximum of at least m
+    __device__ __forceinline__ void rescale(float to) {
+        if (m == to || m == -INFINITY) {
+            m = to;
+            return;
+        }
+        const float t = m - to, f = exp_(t);
+        e = f * fmaf(s, fmaxf(t, kFarBelow), e);
+        s *= f;
+        m = to;
+    }
+};
+
+// PIECES 16-byte pieces of the row a thread holds; 0: the row is read again for
+// the gradient.
+template <typename T, int PIECES, int THREADS>
+__global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a) {
+    constexpr int VEC = 16 / sizeof(T), WAVES = THREADS / 64;
+    __shared__ float red[3][WAVES];
+    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool score = !a.dlogits;
+    const int act = a.actions[r];
+    const float w = !score && a.weights ? a.weights[r] : 1.f;
+    const Row<T> row(static_cast<const T*>(a.logits) + r * a.ld, a.V);
+    const int np = row.pieces();
+    T* out = nullptr;
+    bool same = false;
+    if (!score) {
+        T* p = static_cast<T*>(a.dlogits) + r * a.ld;
+        same = int(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(T)) == row.lo;
+        out = p - row.lo;
+    }
+    auto no_gradient = [&] {
+        if (tid == 0) a.terms[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float zero[VEC] = {};
+        for (int p = tid; p < np; p += THREADS) row.store(out, same, p, zero);
+    };
+    if (act < 0 || (w == 0.f && !a.logp && !a.entropy)) {
+        if (tid == 0 && a.logp) a.logp[r] = 0.f;
+        if (tid == 0 && a.entropy) a.entropy[r] = 0.f;
+        if (!score) no_gradient();
+        return;
+    }
+    const float xa = act < a.V ? to_f(static_cast<const T*>(a.logits)[r * a.ld + act]) : NAN;
+
+    Piece<T> x[PIECES ? PIECES : 1];
+    Soft f;
+    bool nan = false;
+    if constexpr (PIECES > 0) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int p = tid + i * THREADS;
+            if (p < np) {
+                x[i] = row.load(p);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) x[i].set(j, from_f<T>(-INFINITY));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f.m = fmaxf(f.m, x[i].get(j));
+        f.m = wmax(f.m);
+        if (lane == 0) red[0][wave] = f.m;
+        __syncthreads();
+        f.m = red[0][0];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) f.m = fmaxf(f.m, red[0][i]);
+        if (f.m == -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) nan = nan || x[i].get(j) != x[i].get(j);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) f.add(x[i].get(j) - f.m);
+        }
+    } else {
+        for (int p = tid; p < np; p += THREADS) {
+            const Piece<T> v = row.load(p);
+            float m = f.m;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                m = fmaxf(m, v.get(j));
+                nan = nan || v.get(j) != v.get(j);
+            }
+            f.rescale(m);
+            if (m != -INFINITY) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) f.add(v.get(j) - m);
+            }
+        }
+        float m = wmax(f.m);
+        if (lane == 0) red[0][wave] = m;
+        __syncthreads();
+        m = red[0][0];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) m = fmaxf(m, red[0][i]);
+        f.rescale(m);
+    }
+    const bool any_nan = (PIECES == 0 || f.m == -INFINITY) && __syncthreads_or(nan);
+    const float s1 = wsum(f.s), e1 = wsum(f.e);
+    if (lane == 0) red[1][wave] = s1, red[2][wave] = e1;
+    __syncthreads();
+    float S = 0.f, E = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) S += red[1][i], E += red[2][i];
+    const float M = f.m, logS = __builtin_amdgcn_logf(S) * kLn2, inv = 1.f / S;
+    const bool dead = M == -INFINITY && !any_nan && act < a.V;   // nothing to choose from
+    float l = xa - M - logS, H = logS - E * inv;
+    if (dead) l = -INFINITY, H = 0.f;
+    if (any_nan || act >= a.V) l = NAN, H = NAN;
+    if (tid == 0) {
+        if (a.logp) a.logp[r] = l;
+        if (a.entropy) a.entropy[r] = H;
+    }
+    if (score) return;
+    if (w == 0.f) {
+        no_gradient();
+        return;
+    }
+
+    const float ratio = expf(l - a.old_logp[r]), adv = a.adv[r];
+    const float free_ = ratio * adv, cut = fminf(fmaxf(ratio, 1.f - a.lo), 1.f + a.hi) * adv;
+    const bool off = free_ > cut;
+    float c = off ? 0.f : -free_, kl = 0.f;
+    if (a.ref) {
+        const float u = a.ref[r] - l;
+        kl = kl_term(u);
+        c -= a.beta * expm1f(u);
+    }
+    if (tid == 0)
+        a.terms[r] = dead ? make_float4(0.f, 0.f, 0.f, 0.f)
+                          : make_float4(w * -(off ? cut : free_), w * kl, w * H, off ? w : 0.f);
+    const float scale = w / *a.W, cs = rounded_mul(c, scale), es = a.eta * scale, bad = any_nan || act >= a.V ? NAN : 0.f;
+    const int ai = act < a.V ? row.lo + act : -1;
+    auto grad = [&](const Piece<T>& v, int p) {
+        float g[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float t = v.get(j) - M, pj = exp_(t) * inv;
+            g[j] = -cs * pj;
+            if (es != 0.f) g[j] = fmaf(es * pj, fmaxf(t, kFarBelow) - logS + H, g[j]);
+            if (p * VEC + j == ai) g[j] += cs;
+            g[j] = dead ? 0.f : g[j] + bad;
+        }
+        row.store(out, same, p, g);
+    };
+    if constexpr (PIECES > 0) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            if (tid + i * THREADS < np) grad(x[i], tid + i * THREADS);
+    } else {
+        for (int p = tid; p < np; p += THREADS) grad(row.load(p), p);
+    }
+}
+
+// W, one workgroup
+__global__ __launch_bounds__(1024) void policy_weight_kernel(const int32_t* actions, const float* weights, int rows,
+                                                             float* W) {
+    __shared__ double red[16];
+    double s = 0.0;
+    for (int r = threadIdx.x; r < rows; r += 1024)
+        if (actions[r] >= 0) s += weights ? weights[r] : 1.f;
+    s = wsum(s);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = 0.0;
+        for (int i = 0; i < 16; ++i) t += red[i];
+        *W = float(t);
+    }
+}
+
+// the statistics, one workgroup
+__global__ __launch_bounds__(1024) void policy_stats_kernel(PolicyArgs a, float* stats) {
+    __shared__ double red[4][16];
+    double s[4] = {};
+    for (int r = threadIdx.x; r < a.rows; r += 1024) {
+        const float4 t = a.terms[r];
+        s[0] += t.x, s[1] += t.y, s[2] += t.z, s[3] += t.w;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        s[k] = wsum(s[k]);
+        if ((threadIdx.x & 63) == 0) red[k][threadIdx.x >> 6] = s[k];
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const double W = *a.W;
+        for (int k = 0; k < 4; ++k) {
+            s[k] = 0.0;
+            for (int i = 0; i < 16; ++i) s[k] += red[k][i];
+            s[k] = W > 0.0 ? s[k] / W : 0.0;
+        }
+        stats[0] = float(s[0] + (a.ref ? double(a.beta) * s[1] : 0.0) - (a.eta != 0.f ? double(a.eta) * s[2] : 0.0));
+        for (int k = 0; k < 4; ++k) stats[1 + k] = float(s[k]);
+        stats[5] = float(W);
+    }
+}
+
+bool policy_desc_ok(const janus_policy_desc* d) {
+    return d && d->rows > 0 && d->V > 0 && (d->ld == 0 || d->ld >= d->V) && std::isfinite(d->clip_low) &&
+           d->clip_low >= 0.f && std::isfinite(d->clip_high) && d->clip_high >= 0.f && std::isfinite(d->kl_coef) &&
+           std::isfinite(d->ent_coef);
+}
+size_t policy_carve(PolicyArgs& a, float** W, int rows, void* ws) {
+    Carver c(ws);
+    *W = c.take<float>(1);
+    a.W = *W;
+    a.terms = c.take<float4>(rows);
+    return c.off;
+}
+
+template <typename T, int PIECES, int THREADS>
+void row_launch(const PolicyArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((policy_row_kernel<T, PIECES, THREADS>), dim3(a.rows), dim3(THREADS), 0, st, a);
+}
+// The fewest pieces a thread that hold a row (which may touch one piece more than its length fills)
+template <typename T>
+void row_dispatch(const PolicyArgs& a, hipStream_t st) {
+    const int64_t np = (int64_t(a.V) + 16 / sizeof(T) - 2) / (16 / sizeof(T)) + 1;
+    if (np <= 256) row_launch<T, 1, 256>(a, st);
+    else if (np <= 512) row_launch<T, 2, 256>(a, st);
+    else if (np <= 1024) row_launch<T, 4, 256>(a, st);
+    else if (np <= 2048) row_launch<T, 8, 256>(a, st);
+    else if (np <= 4096) row_launch<T, 4, 1024>(a, st);
+    else if (np <= 8192) row_launch<T, 8, 1024>(a, st);
+    else if (np <= 16384) row_launch<T, 16, 1024>(a, st);
+    else row_launch<T, 0, 1024>(a, st);
+}
+
+}  // namespace
+}  // namespace janus
+
+using namespace janus;
+
+extern "C" size_t janus_policy_workspace_bytes(const janus_policy_desc* d) {
+    if (!policy_desc_ok(d) || !dtype_ok(d->dtype)) return 0;
+    PolicyArgs a{};
+    float* W;
+    return policy_carve(a, &W, d->rows, nullptr);
+}
+
+extern "C" janus_status janus_policy_loss(const janus_policy_desc* d, const void* logits, const int32_t* actions,
+                                          const float* old_logp, const float* adv, const float* ref_logp,
+                                          const float* weights, void* dlogits, float* logp, float* entropy,
+                                          float* stats, void* ws, size_t ws_bytes, void* stream) {
+    if (!policy_desc_ok(d) || !logits || !actions) return JANUS_ERR_INVALID_ARG;
+    if (!dtype_ok(d->dtype) || d->V > (1 << 30)) return JANUS_ERR_UNSUPPORTED;
+    const bool score = !dlogits;
+    if (score ? (old_logp || adv || stats) : (!old_logp || !adv)) return JANUS_ERR_INVALID_ARG;
+    const size_t es = dtype_size(d->dtype);
+    if (!aligned(logits, es) || !aligned(dlogits, es) || !aligned(actions, 4)) return JANUS_ERR_INVALID_ARG;
+    for (const float* p : {old_logp, adv, ref_logp, weights, static_cast<const float*>(logp),
+                           static_cast<const float*>(entropy), static_cast<const float*>(stats)})
+        if (!aligned(p, 4)) return JANUS_ERR_INVALID_ARG;
+    PolicyArgs a{};
+    float* W;
+    const size_t need = policy_carve(a, &W, d->rows, ws);
+    if (!score && (!ws || ws_bytes < need || !aligned(ws, 256))) return JANUS_ERR_WORKSPACE;
+    a.rows = d->rows, a.V = d->V, a.ld = d->ld ? d->ld : d->V;
+    a.logits = logits, a.actions = actions, a.old_logp = old_logp, a.adv = adv, a.ref = ref_logp, a.weights = weights;
+    a.dlogits = dlogits, a.logp = logp, a.entropy = entropy;
+    a.lo = d->clip_low, a.hi = d->clip_high, a.beta = d->kl_coef, a.eta = d->ent_coef;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const double el = double(d->rows) * d->V;
+    if (!score) {
+        TraceScope trace("policy_weight", double(d->rows), 8.0 * d->rows, st);
+        hipLaunchKernelGGL(policy_weight_kernel, dim3(1), dim3(1024), 0, st, actions, weights, d->rows, W);
+        JANUS_LAUNCH_CHECK();
+    }
+    {
+        TraceScope trace("policy_row", 9.0 * el, (score ? 1.0 : 2.0) * el * es, st);
+        if (d->dtype == JANUS_BF16) row_dispatch<bf16_t>(a, st);
+        else row_dispatch<float>(a, st);
+        JANUS_LAUNCH_CHECK();
+    }
+    if (stats) {
+        TraceScope trace("policy_stats", 4.0 * d->rows, 16.0 * d->rows, st);
+        hipLaunchKernelGGL(policy_stats_kernel, dim3(1), dim3(1024), 0, st, a, stats);
+        JANUS_LAUNCH_CHECK();
+    }
+    return JANUS_OK;
+}

@@ -1,0 +1,889 @@
+// Selective scan over variable-length sequences: forward, backward, and the
+// single-token step.
+//
+//   e = softplus(dt + dt_bias) (or dt + dt_bias),  u = e x
+//   h_t[n] = exp(e A[n]) h_{t-1}[n] + u B_t[n]
+//   y_t = (sum_n C_t[n] h_t[n] + Dskip x) silu(z)
+//
+// and backward, with gy = dy silu(z) and G_t[n] = dL/dh_t[n]:
+//
+//   G_t[n] = w_{t+1}[n] + gy C_t[n],   w_t[n] = G_t[n] exp(e A[n])
+//   dC_t[n] = sum_d gy h_t[n],   dB_t[n] = sum_d G_t[n] u
+//   s = sum_n G_t[n] B_t[n],  q[n] = w_t[n] h_{t-1}[n],  r = sum_n q[n] A[n]
+//   dx = gy Dskip + e s,  de = x s + r,  dA[n] = sum q[n] e
+//
+// A wave owns 64 channels of one sequence and walks over time.  With few
+// sequences the time axis is cut into segments: a first pass forms each
+// segment's state from a zero start, a small kernel chains them (the decay over
+// a segment is exp(A sum e)), and the second pass starts from the right state.
+// States, decays and every sum over states, time or channels are float32.
+#include "seq.hpp"
+
+namespace janus {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxStates = 64;
+constexpr int kStage = 32;    // steps whose B and C rows lie in LDS at once
+
+// Steps between two kept states: the backward holds the states of one such
+// chunk in registers (128 floats a lane for 16 states and more).
+constexpr int chunk_steps(int NP) { return NP <= 8 ? 16 : 128 / NP; }
+
+struct ScanArgs {
+    int32_t D, N, G, Dg, B, T;
+    int32_t tiles, blocks;    // 64-channel tiles of a group, workgroups of a group
+    int32_t seg, nseg;        // steps per segment (a multiple of kStage), segments
+    int64_t ldx, ldt, ldb, ldc, ldz, ldy;
+    const void *x, *dt, *Bm, *Cm, *z;
+    const float *A, *Dskip, *dtb, *h0;
+    void* y;
+    float* hT;
+    float* ck;        // [chunks - 1][B][NP / 4][D][4] states at the chunks' starts, from the second on
+    float* seg_h;     // [nseg][B][NP / 4][D][4] states at the segments' ends from a zero start, then at their starts
+    float* seg_e;     // [nseg][B][D] sums of e
+    // backward
+    const void* dy;
+    const float* dhT;
+    void *dx, *ddt, *dz, *dBm, *dCm;
+    float* dh0;
+    float* seg_g;     // as seg_h, for G in reverse time
+    float* dA_part;   // [nseg * B][D][N]
+    float* dv_part;   // [nseg * B][2][D] sums of gy x and of ddt
+    float* bc_part;   // [blocks][T * B][G][2][NP], or NULL with one workgroup a group
+    bool softplus;
+};
+
+__device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// log(1 + exp(v)) to a few ulp: with w = exp(-|v|) and s = 1 + w rounded,
+// log1p(w) = log(s) w / (s - 1) (Goldberg, What Every Computer Scientist
+// Should Know About Floating-Point Arithmetic, theorem 4)
+__device__ __forceinline__ float softplus_(float v) {
+    const float w = exp2_(-fabsf(v) * kLog2e), s = 1.f + w, m = s - 1.f;
+    const float l = m == 0.f ? w : __builtin_amdgcn_logf(s) * kLn2 * w * __builtin_amdgcn_rcpf(m);
+    return fmaxf(v, 0.f) + l;
+}
+__device__ __forceinline__ float step_size(float v, bool softplus) { return softplus ? softplus_(v) : v; }
+
+// [seg or chunk][b][quarter][d][4]
+template <int NP>
+__device__ __forceinline__ float* state_at(float* p, const ScanArgs& a, int64_t i, int b, int q, int d) {
+    return p + (((i * a.B + b) * (NP / 4) + q) * a.D + d) * 4;
+}
+
+// Rows [t, t + n) of B and C as float32 in LDS, [step][B, C][NP]; zero past
+// the sequence's end and past N.
+template <typename T, int NP>
+__device__ __forceinline__ void stage_bc(const ScanArgs& a, float* lds, int t, int n, int te, int b, int group) {
+    for (int i = threadIdx.x; i < n * 2 * NP; i += blockDim.x) {
+        const int st = i / (2 * NP), k = i % (2 * NP), m = k % NP;
+        float v = 0.f;
+        if (t + st < te && m < a.N) {
+            const int64_t r = int64_t(t + st) * a.B + b;
+            v = k < NP ? to_f(static_cast<const T*>(a.Bm)[r * a.ldb + int64_t(group) * a.N + m])
+                       : to_f(static_cast<const T*>(a.Cm)[r * a.ldc + int64_t(group) * a.N + m]);
+        }
+        lds[i] = v;
+    }
+}
+
+// One lane per channel, its NP states in registers; B and C come from LDS,
+// the same address in all lanes.  LOCAL: only the state at the segment's end
+// from a zero start, and the sum of e.
+template <typename T, int NP, bool LOCAL>
+__global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
+    constexpr int CK = chunk_steps(NP), U = 8;
+    __shared__ float bc[kStage * 2 * NP];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int group = blockIdx.x / a.blocks, tile = (blockIdx.x % a.blocks) * waves + wave;
+    const int ch = tile * 64 + lane;
+    const bool live = ch < a.Dg;
+    const int d = group * a.Dg + (live ? ch : 0);
+    const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
+    const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg), te = min(t1, len);
+    float A2[NP], h[NP];
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+        A2[n] = n < a.N ? a.A[int64_t(d) * a.N + n] * kLog2e : 0.f;
+        h[n] = 0.f;
+    }
+    if (!LOCAL && seg > 0) {
+#pragma unroll
+        for (int q = 0; q < NP / 4; ++q) {
+            const float4 v = *reinterpret_cast<const float4*>(state_at<NP>(a.seg_h, a, seg, b, q, d));
+            h[4 * q] = v.x, h[4 * q + 1] = v.y, h[4 * q + 2] = v.z, h[4 * q + 3] = v.w;
+        }
+    } else if (!LOCAL && a.h0) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            if (n < a.N) h[n] = a.h0[(int64_t(b) * a.D + d) * a.N + n];
+    }
+    const float dskip = a.Dskip ? a.Dskip[d] : 0.f, dtb = a.dtb ? a.dtb[d] : 0.f;
+    const T* xp = static_cast<const T*>(a.x) + b * a.ldx + d;
+    const T* tp = static_cast<const T*>(a.dt) + b * a.ldt + d;
+    const T* zp = a.z ? static_cast<const T*>(a.z) + b * a.ldz + d : nullptr;
+    T* yp = LOCAL ? nullptr : static_cast<T*>(a.y) + b * a.ldy + d;
+    const int64_t sx = a.B * a.ldx, st = a.B * a.ldt, sz = a.B * a.ldz, sy = a.B * a.ldy;
+    float esum = 0.f;
+    for (int ts = t0; ts < te; ts += kStage) {
+        __syncthreads();
+        stage_bc<T, NP>(a, bc, ts, min(kStage, te - ts), te, b, group);
+        __syncthreads();
+        for (int tu = ts; tu < min(te, ts + kStage); tu += U) {
+            T rx[U], rt[U], rz[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                if (tu + i < te && live) {
+                    rx[i] = xp[(tu + i) * sx];
+                    rt[i] = tp[(tu + i) * st];
+                    if (!LOCAL && zp) rz[i] = zp[(tu + i) * sz];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int t = tu + i;
+                if (t >= te) break;
+                if (!LOCAL && a.ck && t % CK == 0 && t > 0 && live) {
+#pragma unroll
+                    for (int q = 0; q < NP / 4; ++q)
+                        *reinterpret_cast<float4*>(state_at<NP>(a.ck, a, t / CK - 1, b, q, d)) =
+                            make_float4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+                }
+                const float x = to_f(rx[i]), e = step_size(to_f(rt[i]) + dtb, a.softplus), u = e * x;
+                const float* row = bc + (t - ts) * 2 * NP;
+                float y = 0.f;
+#pragma unroll
+                for (int n = 0; n < NP; ++n) {
+                    h[n] = fmaf(exp2_(e * A2[n]), h[n], u * row[n]);
+                    if (!LOCAL) y = fmaf(h[n], row[NP + n], y);
+                }
+                if (LOCAL) {
+                    esum += e;
+                } else if (live) {
+                    y = fmaf(dskip, x, y);
+                    if (zp) {
+                        const float z = to_f(rz[i]);
+                        y *= z * sigmoidf_(z);
+                    }
+                    yp[t * sy] = from_f<T>(y);
+                }
+            }
+        }
+    }
+    if (!live) return;
+    if (LOCAL) {
+#pragma unroll
+        for (int q = 0; q < NP / 4; ++q)
+            *reinterpret_cast<float4*>(state_at<NP>(a.seg_h, a, seg, b, q, d)) =
+                make_float4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+        a.seg_e[(int64_t(seg) * a.B + b) * a.D + d] = esum;
+        return;
+    }
+    for (int t = max(t0, len); t < t1; ++t) yp[t * sy] = from_f<T>(0.f);
+    if (a.hT && seg == a.nseg - 1) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            if (n < a.N) a.hT[(int64_t(b) * a.D + d) * a.N + n] = h[n];
+    }
+}
+
+// The other direction of LOCAL: G at a segment's start from a zero end,
+// without its own... the part that flows into the segment before it.
+template <typename T, int NP>
+__global__ __launch_bounds__(256) void scan_rev_kernel(ScanArgs a, SeqSlice s) {
+    constexpr int U = 8;
+    __shared__ float bc[kStage * 2 * NP];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int group = blockIdx.x / a.blocks, tile = (blockIdx.x % a.blocks) * waves + wave;
+    const int ch = tile * 64 + lane;
+    const bool live = ch < a.Dg;
+    const int d = group * a.Dg + (live ? ch : 0);
+    const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
+    const int t0 = seg * a.seg, te = min(min(a.T, t0 + a.seg), len);
+    float A2[NP], g[NP];
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+        A2[n] = n < a.N ? a.A[int64_t(d) * a.N + n] * kLog2e : 0.f;
+        g[n] = 0.f;
+    }
+    const float dtb = a.dtb ? a.dtb[d] : 0.f;
+    const T* tp = static_cast<const T*>(a.dt) + b * a.ldt + d;
+    const T* zp = a.z ? static_cast<const T*>(a.z) + b * a.ldz + d : nullptr;
+    const T* gp = static_cast<const T*>(a.dy) + b * a.ldy + d;
+    const int64_t st = a.B * a.ldt, sz = a.B * a.ldz, sy = a.B * a.ldy;
+    const int n_stage = te > t0 ? (te - t0 + kStage - 1) / kStage : 0;
+    for (int k = n_stage - 1; k >= 0; --k) {
+        const int ts = t0 + k * kStage, tn = min(te, ts + kStage);
+        __syncthreads();
+        stage_bc<T, NP>(a, bc, ts, tn - ts, te, b, group);
+        __syncthreads();
+        for (int tu = tn; tu > ts; tu -= U) {   // steps tu - 1 down to tu - U
+            T rt[U], rz[U], rg[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int t = tu - 1 - i;
+                if (t >= ts && live) {
+                    rt[i] = tp[t * st];
+                    rg[i] = gp[t * sy];
+                    if (zp) rz[i] = zp[t * sz];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int t = tu - 1 - i;
+                if (t < ts) break;
+                const float e = step_size(to_f(rt[i]) + dtb, a.softplus);
+                float gy = to_f(rg[i]);
+                if (zp) {
+                    const float z = to_f(rz[i]);
+                    gy *= z * sigmoidf_(z);
+                }
+                const float* row = bc + (t - ts) * 2 * NP + NP;
+#pragma unroll
+                for (int n = 0; n < NP; ++n) g[n] = fmaf(gy, row[n], g[n]) * exp2_(e * A2[n]);
+            }
+        }
+    }
+    if (!live) return;
+#pragma unroll
+    for (int q = 0; q < NP / 4; ++q)
+        *reinterpret_cast<float4*>(state_at<NP>(a.seg_g, a, seg, b, q, d)) =
+            make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]);
+}
+
+// Chains the segments.  forward: seg_h[i] becomes the state at segment i's
+// start; reverse: seg_g[i] becomes what flows into segment i's end.
+template <int NP, bool REVERSE>
+__global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
+    const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;   // (b, quarter, d)
+    if (i >= int64_t(a.B) * (NP / 4) * a.D) return;
+    const int d = int(i % a.D), q = int(i / a.D % (NP / 4)), b = int(i / a.D / (NP / 4));
+    const float* first = REVERSE ? a.dhT : a.h0;
+    float A2[4], h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = 4 * q + j;
+        A2[j] = n < a.N ? a.A[int64_t(d) * a.N + n] * kLog2e : 0.f;
+        h[j] = n < a.N && first ? first[(int64_t(b) * a.D + d) * a.N + n] : 0.f;
+    }
+    for (int k = 0; k < a.nseg; ++k) {
+        const int seg = REVERSE ? a.nseg - 1 - k : k;
+        float4* p = reinterpret_cast<float4*>(state_at<NP>(REVERSE ? a.seg_g : a.seg_h, a, seg, b, q, d));
+        const float e = a.seg_e[(int64_t(seg) * a.B + b) * a.D + d];
+        const float4 v = *p;
+        *p = make_float4(h[0], h[1], h[2], h[3]);
+        h[0] = fmaf(exp2_(e * A2[0]), h[0], v.x);
+        h[1] = fmaf(exp2_(e * A2[1]), h[1], v.y);
+        h[2] = fmaf(exp2_(e * A2[2]), h[2], v.z);
+        h[3] = fmaf(exp2_(e * A2[3]), h[3], v.w);
+    }
+}
+
+// ------------------------------------------------------------ lane exchange
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// Sums of a in the lanes of even 16-lane rows, of b in the odd ones, each over
+// two neighbouring rows
+__device__ __forceinline__ float fold16(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// the same for the two halves of the wave
+__device__ __forceinline__ float fold32(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// v[r] summed over the four 16-lane rows; row r keeps v[r]
+__device__ __forceinline__ float fold_rows(const float (&v)[4]) { return fold32(fold16(v[0], v[1]), fold16(v[2], v[3])); }
+
+// M values summed over the 16 lanes of a row.  Where there are values left to
+// share, each step leaves a lane with half of them (which half: a bit of the
+// lane's number); then it sums.  Lane l ends with values first(l) + [0, max(1, M / 16)).
+template <int M>
+struct RowFold {
+    static constexpr int left = M > 16 ? M / 16 : 1;
+    template <int CTRL, int BIT, int m>
+    __device__ __forceinline__ static void step(float* v, int lane) {
+        if constexpr (m > 1) {
+            const bool up = lane & BIT;
+#pragma unroll
+            for (int i = 0; i < m / 2; ++i) {
+                const float keep = up ? v[i + m / 2] : v[i], give = up ? v[i] : v[i + m / 2];
+                v[i] = keep + dpp<CTRL>(give);
+            }
+        } else {
+            v[0] += dpp<CTRL>(v[0]);
+        }
+    }
+    // row_ror:8 meets lane l ^ 8; row_half_mirror l ^ 7, whose bit 4 differs; then l ^ 2 and l ^ 1
+    __device__ __forceinline__ static void run(float* v, int lane) {
+        step<0x128, 8, M>(v, lane);
+        step<0x141, 4, (M > 2 ? M / 2 : 1)>(v, lane);
+        step<0x4e, 2, (M > 4 ? M / 4 : 1)>(v, lane);
+        step<0xb1, 1, (M > 8 ? M / 8 : 1)>(v, lane);
+    }
+    __device__ __forceinline__ static int first(int lane) {
+        int i = (lane & 8) ? M / 2 : 0;
+        if (M > 2 && (lane & 4)) i += M / 4;
+        if (M > 4 && (lane & 2)) i += M / 8;
+        if (M > 8 && (lane & 1)) i += M / 16;
+        return i;
+    }
+    // of the lanes with equal values, one writes them
+    __device__ __forceinline__ static bool writes(int lane) {
+        return M >= 16 || (lane & (M == 8 ? 1 : M == 4 ? 3 : 7)) == 0;
+    }
+};
+
+// Backward of one segment.  A wave's 64 channels lie 4 to a lane (lane l: channels
+// 4 (l % 16) + [0, 4)) and the states in four parts over the wave's 16-lane
+// rows, so the sums over channels that dB and dC need are mostly in-lane, and
+// the sums over states cost six operations for four channels.  fold_rows leaves
+// lane l with channel 4 (l % 16) + l / 16, for which it does the work per
+// channel (step size, gate, stores); values cross between the two layouts in LDS.
+// Chunks go backwards; the states inside one are formed again from its start.
+template <typename T, int NP, bool GATE>
+__global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a, SeqSlice s) {
+    constexpr int CK = chunk_steps(NP), NL = NP / 4, W = 4;
+    __shared__ float bc[CK * 2 * NP];
+    __shared__ float red[W][CK][2 * NP];
+    __shared__ float sh[W][GATE ? 6 : 5][CK][64];   // e, u, gy, x, de/dv, and with a gate dy silu'(z)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int c16 = lane & 15, ng = lane >> 4;
+    const int group = blockIdx.x / a.blocks, blk = blockIdx.x % a.blocks, tile = blk * waves + wave;
+    const int own = 4 * c16 + ng;
+    const bool live = tile * 64 + own < a.Dg;
+    const int d = group * a.Dg + (live ? tile * 64 + own : 0);
+    const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
+    const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg);
+    float A2[4][NL], g[4][NL], dA[4][NL];
+    int dc[4];   // the lane's channels in the state layout, and whether they exist
+    bool dl[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int ch = tile * 64 + 4 * c16 + r;
+        dl[r] = ch < a.Dg;
+        dc[r] = group * a.Dg + (dl[r] ? ch : 0);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int n = ng * NL + i;
+            const bool on = dl[r] && n < a.N;
+            A2[r][i] = on ? a.A[int64_t(dc[r]) * a.N + n] * kLog2e : 0.f;
+            dA[r][i] = 0.f;
+            g[r][i] = 0.f;
+            if (on) {
+                if (a.nseg > 1) g[r][i] = state_at<NP>(a.seg_g, a, seg, b, n / 4, dc[r])[n % 4];
+                else if (a.dhT) g[r][i] = a.dhT[(int64_t(b) * a.D + dc[r]) * a.N + n];
+            }
+        }
+    }
+    const float dskip = a.Dskip ? a.Dskip[d] : 0.f, dtb = a.dtb ? a.dtb[d] : 0.f;
+    const T* xp = static_cast<const T*>(a.x) + b * a.ldx + d;
+    const T* tp = static_cast<const T*>(a.dt) + b * a.ldt + d;
+    const T* zp = GATE ? static_cast<const T*>(a.z) + b * a.ldz + d : nullptr;
+    const T* gp = static_cast<const T*>(a.dy) + b * a.ldy + d;
+    T* dxp = static_cast<T*>(a.dx) + b * a.ldx + d;
+    T* dtp = static_cast<T*>(a.ddt) + b * a.ldt + d;
+    T* dzp = GATE ? static_cast<T*>(a.dz) + b * a.ldz + d : nullptr;
+    const int64_t sx = a.B * a.ldx, st = a.B * a.ldt, sz = a.B * a.ldz, sy = a.B * a.ldy;
+    float dD = 0.f, dtbs = 0.f;
+    for (int tc = t0 + (t1 - 1 - t0) / CK * CK; tc >= t0; tc -= CK) {
+        const int tn = min(CK, t1 - tc);
+        if (tc < len) {
+            // the work per channel of the chunk's steps
+#pragma unroll
+            for (int i = 0; i < CK; ++i) {
+                float e = 0.f, u = 0.f, gy = 0.f, x = 0.f, sv = 0.f, zf = 0.f;
+                if (tc + i < min(len, t1) && live) {
+                    x = to_f(xp[(tc + i) * sx]);
+                    const float v = to_f(tp[(tc + i) * st]) + dtb;
+                    e = step_size(v, a.softplus);
+                    sv = a.softplus ? sigmoidf_(v) : 1.f;
+                    u = e * x;
+                    gy = to_f(gp[(tc + i) * sy]);
+                    if (GATE) {
+                        const float z = to_f(zp[(tc + i) * sz]), q = sigmoidf_(z);
+                        zf = gy * q * (1.f + z * (1.f - q));
+                        gy *= z * q;
+                    }
+                }
+                sh[wave][0][i][own] = e;
+                sh[wave][1][i][own] = u;
+                sh[wave][2][i][own] = gy;
+                sh[wave][3][i][own] = x;
+                sh[wave][4][i][own] = sv;
+                if (GATE) sh[wave][GATE ? 5 : 0][i][own] = zf;
+            }
+            stage_bc<T, NP>(a, bc, tc, CK, min(len, t1), b, group);
+        }
+        __syncthreads();
+        if (tc < len) {
+            // states of the chunk: h[i] before its step i
+            float h[CK + 1][4][NL];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const int n = ng * NL + i;
+                    h[0][r][i] = 0.f;
+                    if (dl[r] && n < a.N) {
+                        if (tc > 0) h[0][r][i] = state_at<NP>(a.ck, a, tc / CK - 1, b, n / 4, dc[r])[n % 4];
+                        else if (a.h0) h[0][r][i] = a.h0[(int64_t(b) * a.D + dc[r]) * a.N + n];
+                    }
+                }
+#pragma unroll
+            for (int k = 0; k < CK; ++k) {
+                const float4 e4 = *reinterpret_cast<const float4*>(&sh[wave][0][k][4 * c16]);
+                const float4 u4 = *reinterpret_cast<const float4*>(&sh[wave][1][k][4 * c16]);
+                const float e[4] = {e4.x, e4.y, e4.z, e4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const float bn = bc[k * 2 * NP + ng * NL + i];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) h[k + 1][r][i] = fmaf(exp2_(e[r] * A2[r][i]), h[k][r][i], u[r] * bn);
+                }
+            }
+#pragma unroll
+            for (int k = CK - 1; k >= 0; --k) {
+                const float4 e4 = *reinterpret_cast<const float4*>(&sh[wave][0][k][4 * c16]);
+                const float4 u4 = *reinterpret_cast<const float4*>(&sh[wave][1][k][4 * c16]);
+                const float4 g4 = *reinterpret_cast<const float4*>(&sh[wave][2][k][4 * c16]);
+                const float e[4] = {e4.x, e4.y, e4.z, e4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+                const float gy[4] = {g4.x, g4.y, g4.z, g4.w};
+                float bcs[2 * NL], sb[4] = {}, sa[4] = {}, yr[4] = {};
+#pragma unroll
+                for (int i = 0; i < 2 * NL; ++i) bcs[i] = 0.f;
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const float bn = bc[k * 2 * NP + ng * NL + i], cn = bc[k * 2 * NP + NP + ng * NL + i];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float gn = fmaf(gy[r], cn, g[r][i]);
+                        bcs[NL + i] = fmaf(gy[r], h[k + 1][r][i], bcs[NL + i]);
+                        bcs[i] = fmaf(gn, u[r], bcs[i]);
+                        sb[r] = fmaf(gn, bn, sb[r]);
+                        if (GATE) yr[r] = fmaf(h[k + 1][r][i], cn, yr[r]);
+                        const float w = gn * exp2_(e[r] * A2[r][i]), q = w * h[k][r][i];
+                        sa[r] = fmaf(q, A2[r][i], sa[r]);
+                        dA[r][i] = fmaf(q, e[r], dA[r][i]);
+                        g[r][i] = w;
+                    }
+                }
+                RowFold<2 * NL>::run(bcs, lane);
+                if (RowFold<2 * NL>::writes(lane)) {
+                    const int f = RowFold<2 * NL>::first(c16);
+#pragma unroll
+                    for (int j = 0; j < RowFold<2 * NL>::left; ++j) {
+                        const int m = f + j;   // states NL of dB, then of dC
+                        red[wave][k][(m < NL ? 0 : NP - NL) + ng * NL + m] = bcs[j];
+                    }
+                }
+                const float S = fold_rows(sb), R = fold_rows(sa) * kLn2;
+                const float oe = sh[wave][0][k][own], ogy = sh[wave][2][k][own], ox = sh[wave][3][k][own];
+                const float ddt = (ox * S + R) * sh[wave][4][k][own];
+                dD += ogy * ox;
+                dtbs += ddt;
+                float dz = 0.f;
+                if (GATE) dz = sh[wave][GATE ? 5 : 0][k][own] * fmaf(dskip, ox, fold_rows(yr));
+                if (k < tn && live) {   // 0 past the sequence's end: e, u, gy, x are
+                    dxp[(tc + k) * sx] = from_f<T>(fmaf(ogy, dskip, oe * S));
+                    dtp[(tc + k) * st] = from_f<T>(ddt);
+                    if (GATE) dzp[(tc + k) * sz] = from_f<T>(dz);
+                }
+            }
+        } else if (live) {
+            for (int k = 0; k < tn; ++k) {
+                dxp[(tc + k) * sx] = from_f<T>(0.f);
+                dtp[(tc + k) * st] = from_f<T>(0.f);
+                if (GATE) dzp[(tc + k) * sz] = from_f<T>(0.f);
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < tn * 2 * NP; i += blockDim.x) {
+            const int k = i / (2 * NP), m = i % (2 * NP), n = m % NP;
+            float v = 0.f;
+            if (tc + k < len)
+                for (int w = 0; w < waves; ++w) v += red[w][k][m];
+            const int64_t row = int64_t(tc + k) * a.B + b;
+            if (a.bc_part) {
+                a.bc_part[((int64_t(blk) * a.T * a.B + row) * a.G + group) * 2 * NP + m] = v;
+            } else if (n < a.N) {
+                if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = from_f<T>(v);
+                else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = from_f<T>(v);
+            }
+        }
+    }
+    const int64_t part = int64_t(seg) * a.B + b;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int n = ng * NL + i;
+            if (!dl[r] || n >= a.N) continue;
+            a.dA_part[(part * a.D + dc[r]) * a.N + n] = dA[r][i];
+            if (a.dh0 && seg == 0) a.dh0[(int64_t(b) * a.D + dc[r]) * a.N + n] = g[r][i];
+        }
+    if (live) {
+        a.dv_part[part * 2 * a.D + d] = dD;
+        a.dv_part[(part * 2 + 1) * a.D + d] = dtbs;
+    }
+}
+
+// dA, dDskip, ddt_bias: the parts summed in their order
+__global__ __launch_bounds__(64) void scan_param_kernel(const float* dA_part, const float* dv_part, int parts, int D,
+                                                        int N, float* dA, float* dD, float* ddtb) {
+    const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, na = int64_t(D) * N;
+    if (i >= na + 2 * D) return;
+    const float* p = i < na ? dA_part + i : dv_part + (i - na);
+    const int64_t step = i < na ? na : 2 * int64_t(D);
+    float v = 0.f;
+    for (int k = 0; k < parts; ++k) v += p[k * step];
+    if (i < na) dA[i] = v;
+    else if (i < na + D) {
+        if (dD) dD[i - na] = v;
+    } else if (ddtb) {
+        ddtb[i - na - D] = v;
+    }
+}
+
+// dB and dC: the workgroups' parts of each row
+template <typename T, int NP>
+__global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a) {
+    const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, rows = int64_t(a.T) * a.B;
+    const int64_t all = rows * a.G * 2 * NP;
+    if (i >= all) return;
+    const int m = int(i % (2 * NP)), n = m % NP, group = int(i / (2 * NP) % a.G);
+    const int64_t row = i / (2 * NP) / a.G;
+    if (n >= a.N) return;
+    float v = 0.f;
+    for (int k = 0; k < a.blocks; ++k) v += a.bc_part[k * all + i];
+    if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = from_f<T>(v);
+    else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = from_f<T>(v);
+}
+
+// One token: QL lanes per channel with 4 states each.
+template <typename T, int QL, bool VEC4>
+__global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, const int32_t* slots, int32_t n_slots,
+                                                        float* state) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x, q = i % QL, d0 = i / QL, b = blockIdx.y;
+    const bool live = d0 < a.D;
+    const int d = live ? d0 : 0;
+    const int slot = slots ? slots[b] : b;
+    T* yp = static_cast<T*>(a.y) + b * a.ldy + d;
+    if (slot < 0 || slot >= n_slots) {
+        if (live && q == 0) *yp = from_f<T>(0.f);
+        return;
+    }
+    const int n0 = 4 * q, group = d / a.Dg;
+    float* sp = state + (int64_t(slot) * a.D + d) * a.N + n0;
+    float h[4] = {}, A[4] = {}, bn[4] = {}, cn[4] = {};
+    const float* ap = a.A + int64_t(d) * a.N + n0;
+    const T* bp = static_cast<const T*>(a.Bm) + b * a.ldb + int64_t(group) * a.N + n0;
+    const T* cp = static_cast<const T*>(a.Cm) + b * a.ldc + int64_t(group) * a.N + n0;
+    if (VEC4) {
+        if (n0 < a.N) {
+            const float4 v = *reinterpret_cast<const float4*>(sp), w = *reinterpret_cast<const float4*>(ap);
+            h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
+            A[0] = w.x, A[1] = w.y, A[2] = w.z, A[3] = w.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (n0 + j < a.N) h[j] = sp[j], A[j] = ap[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (n0 + j < a.N) bn[j] = to_f(bp[j]), cn[j] = to_f(cp[j]);
+    const float x = to_f(static_cast<const T*>(a.x)[b * a.ldx + d]);
+    const float e = step_size(to_f(static_cast<const T*>(a.dt)[b * a.ldt + d]) + (a.dtb ? a.dtb[d] : 0.f), a.softplus);
+    float y = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        h[j] = fmaf(exp2_(e * A[j] * kLog2e), h[j], e * x * bn[j]);
+        y = fmaf(h[j], cn[j], y);
+    }
+    if (live) {
+        if (VEC4) {
+            if (n0 < a.N) *reinterpret_cast<float4*>(sp) = make_float4(h[0], h[1], h[2], h[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n0 + j < a.N) sp[j] = h[j];
+        }
+    }
+#pragma unroll
+    for (int o = QL / 2; o > 0; o >>= 1) y += __shfl_xor(y, o, 64);
+    if (live && q == 0) {
+        y = fmaf(a.Dskip ? a.Dskip[d] : 0.f, x, y);
+        if (a.z) {
+            const float z = to_f(static_cast<const T*>(a.z)[b * a.ldz + d]);
+            y *= z * sigmoidf_(z);
+        }
+        *yp = from_f<T>(y);
+    }
+}
+
+// -------------------------------------------------------------------- host
+bool scan_desc_ok(const janus_scan_desc* d) {
+    if (!d || d->D <= 0 || d->N <= 0 || d->G <= 0 || d->B <= 0 || d->T < 0 || d->D % d->G != 0) return false;
+    for (int64_t ld : {d->ldx, d->ldt, d->ldz, d->ldy})
+        if (ld != 0 && ld < d->D) return false;
+    for (int64_t ld : {d->ldb, d->ldc})
+        if (ld != 0 && ld < int64_t(d->G) * d->N) return false;
+    return true;
+}
+bool scan_supported(const janus_scan_desc* d) {
+    return dtype_ok(d->dtype) && d->N <= kMaxStates && (d->flags & ~(JANUS_SCAN_SOFTPLUS | JANUS_SCAN_KEEP)) == 0 &&
+           d->T <= (1 << 30) && d->D <= (1 << 24) && d->B <= (1 << 24);
+}
+// states rounded up to what the kernels are built for
+int padded_states(int N) { return N <= 4 ? 4 : N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
+
+constexpr int kScanWaves = 4;
+
+// The geometry of a descriptor: a function of it alone, so that the forward,
+// the backward and the workspace agree.
+ScanArgs scan_geometry(const janus_scan_desc* d) {
+    ScanArgs a{};
+    a.D = d->D, a.N = d->N, a.G = d->G, a.Dg = d->D / d->G, a.B = d->B, a.T = d->T;
+    a.ldx = d->ldx ? d->ldx : d->D, a.ldt = d->ldt ? d->ldt : d->D, a.ldz = d->ldz ? d->ldz : d->D;
+    a.ldy = d->ldy ? d->ldy : d->D;
+    a.ldb = d->ldb ? d->ldb : int64_t(d->G) * d->N, a.ldc = d->ldc ? d->ldc : int64_t(d->G) * d->N;
+    a.softplus = d->flags & JANUS_SCAN_SOFTPLUS;
+    a.tiles = (a.Dg + 63) / 64;
+    a.blocks = (a.tiles + kScanWaves - 1) / kScanWaves;
+    // With fewer waves than the chip's 1024 SIMDs the time axis is cut, into segments of 64 steps
+    // and more, for two waves a SIMD: the cut costs a second pass over the inputs.
+    const int64_t waves = int64_t(a.B) * a.G * a.tiles;
+    int64_t want = 1;
+    if (waves < 1024) want = std::max<int64_t>(1, std::min<int64_t>((2048 + waves - 1) / waves, a.T / 64));
+    a.seg = int(std::max<int64_t>(kStage, round_up((a.T + want - 1) / want, kStage)));
+    a.nseg = std::max(1, (a.T + a.seg - 1) / a.seg);
+    return a;
+}
+// workspace regions (sizes only with ws NULL)
+size_t scan_carve(ScanArgs& a, bool keep, void* ws) {
+    const int NP = padded_states(a.N), CK = chunk_steps(NP);
+    const size_t state = size_t(a.B) * NP * a.D;
+    Carver c(ws);
+    if (a.nseg > 1) {
+        a.seg_h = c.take<float>(a.nseg * state);
+        a.seg_e = c.take<float>(size_t(a.nseg) * a.B * a.D);
+    }
+    if (keep) {
+        const size_t chunks = size_t((a.T + CK - 1) / CK), parts = size_t(a.nseg) * a.B;
+        a.ck = c.take<float>((chunks ? chunks - 1 : 0) * state);
+        if (a.nseg > 1) a.seg_g = c.take<float>(a.nseg * state);
+        a.dA_part = c.take<float>(parts * a.D * a.N);
+        a.dv_part = c.take<float>(parts * 2 * a.D);
+        if (a.blocks > 1) a.bc_part = c.take<float>(size_t(a.blocks) * a.T * a.B * a.G * 2 * NP);
+    }
+    return c.off;
+}
+janus_status scan_check(const janus_scan_desc* d, const void* x, const void* dt, const float* A, const void* Bm,
+                        const void* Cm, const float* Dskip, const void* z, const float* dt_bias, const void* y,
+                        bool rows) {
+    if (!scan_desc_ok(d) || !A || (rows && (!x || !dt || !Bm || !Cm || !y))) return JANUS_ERR_INVALID_ARG;
+    if (!scan_supported(d)) return JANUS_ERR_UNSUPPORTED;
+    const size_t es = dtype_size(d->dtype);
+    for (const void* p : {x, dt, Bm, Cm, z, y})
+        if (!aligned(p, es)) return JANUS_ERR_INVALID_ARG;
+    for (const float* p : {A, Dskip, dt_bias})
+        if (!aligned(p, 4)) return JANUS_ERR_INVALID_ARG;
+    if (y && (y == x || y == dt || y == z || y == Bm || y == Cm)) return JANUS_ERR_INVALID_ARG;
+    return JANUS_OK;
+}
+void scan_inputs(ScanArgs& a, const void* x, const void* dt, const float* A, const void* Bm, const void* Cm,
+                 const float* Dskip, const void* z, const float* dt_bias) {
+    a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.Dskip = Dskip, a.z = z, a.dtb = dt_bias;
+}
+
+dim3 scan_block(const ScanArgs& a) { return dim3(64 * std::min(kScanWaves, a.tiles)); }
+
+template <typename T, int NP>
+janus_status scan_fwd_run(const ScanArgs& a, const int32_t* lengths, hipStream_t st) {
+    const double el = double(a.T) * a.B * a.D;
+    if (a.nseg > 1) {
+        for (int32_t b0 = 0; b0 < a.B; b0 += kSlice) {
+            SeqSlice s;
+            const int n = fill_slice(s, b0, a.B, a.T, lengths);
+            TraceScope trace("scan_fwd_local", el / a.B * n * 5 * a.N, el / a.B * n * 2 * sizeof(T), st);
+            hipLaunchKernelGGL((scan_fwd_kernel<T, NP, true>), dim3(a.blocks * a.G, n, a.nseg), scan_block(a), 0, st, a,
+                               s);
+            JANUS_LAUNCH_CHECK();
+        }
+        const int64_t all = int64_t(a.B) * (NP / 4) * a.D;
+        TraceScope trace("scan_chain", 8.0 * all * a.nseg, 36.0 * all * a.nseg, st);
+        hipLaunchKernelGGL((scan_chain_kernel<NP, false>), dim3((all + 255) / 256), dim3(256), 0, st, a);
+        JANUS_LAUNCH_CHECK();
+    }
+    for (int32_t b0 = 0; b0 < a.B; b0 += kSlice) {
+        SeqSlice s;
+        const int n = fill_slice(s, b0, a.B, a.T, lengths);
+        TraceScope trace("scan_fwd", el / a.B * n * 7 * a.N, el / a.B * n * (a.z ? 4 : 3) * sizeof(T), st);
+        hipLaunchKernelGGL((scan_fwd_kernel<T, NP, false>), dim3(a.blocks * a.G, n, a.nseg), scan_block(a), 0, st, a, s);
+        JANUS_LAUNCH_CHECK();
+    }
+    return JANUS_OK;
+}
+
+template <typename T, int NP>
+janus_status scan_bwd_run(const ScanArgs& a, const int32_t* lengths, float* dA, float* dDskip, float* ddt_bias,
+                          hipStream_t st) {
+    const double el = double(a.T) * a.B * a.D;
+    if (a.nseg > 1) {
+        for (int32_t b0 = 0; b0 < a.B; b0 += kSlice) {
+            SeqSlice s;
+            const int n = fill_slice(s, b0, a.B, a.T, lengths);
+            TraceScope trace("scan_bwd_local", el / a.B * n * 5 * a.N, el / a.B * n * 3 * sizeof(T), st);
+            hipLaunchKernelGGL((scan_rev_kernel<T, NP>), dim3(a.blocks * a.G, n, a.nseg), scan_block(a), 0, st, a, s);
+            JANUS_LAUNCH_CHECK();
+        }
+        const int64_t all = int64_t(a.B) * (NP / 4) * a.D;
+        TraceScope trace("scan_chain", 8.0 * all * a.nseg, 36.0 * all * a.nseg, st);
+        hipLaunchKernelGGL((scan_chain_kernel<NP, true>), dim3((all + 255) / 256), dim3(256), 0, st, a);
+        JANUS_LAUNCH_CHECK();
+    }
+    for (int32_t b0 = 0; b0 < a.B; b0 += kSlice) {
+        SeqSlice s;
+        const int n = fill_slice(s, b0, a.B, a.T, lengths);
+        TraceScope trace("scan_bwd", el / a.B * n * 24 * a.N, el / a.B * n * (a.z ? 7 : 5) * sizeof(T), st);
+        const dim3 grid(a.blocks * a.G, n, a.nseg);
+        if (a.z) hipLaunchKernelGGL((scan_bwd_kernel<T, NP, true>), grid, scan_block(a), 0, st, a, s);
+        else hipLaunchKernelGGL((scan_bwd_kernel<T, NP, false>), grid, scan_block(a), 0, st, a, s);
+        JANUS_LAUNCH_CHECK();
+    }
+    const int64_t np = int64_t(a.D) * a.N + 2 * a.D;
+    {
+        const int parts = a.nseg * a.B;
+        TraceScope trace("scan_param", double(np) * parts, 4.0 * np * parts, st);
+        hipLaunchKernelGGL(scan_param_kernel, dim3((np + 63) / 64), dim3(64), 0, st, a.dA_part, a.dv_part, parts, a.D,
+                           a.N, dA, dDskip, ddt_bias);
+        JANUS_LAUNCH_CHECK();
+    }
+    if (a.bc_part && a.T > 0) {
+        const int64_t all = int64_t(a.T) * a.B * a.G * 2 * NP;
+        TraceScope trace("scan_bc", double(all) * a.blocks, 4.0 * all * a.blocks, st);
+        hipLaunchKernelGGL((scan_bc_kernel<T, NP>), dim3((all + 255) / 256), dim3(256), 0, st, a);
+        JANUS_LAUNCH_CHECK();
+    }
+    return JANUS_OK;
+}
+
+template <template <typename, int> class F, typename T, class... P>
+janus_status with_states(int N, P&&... p) {
+    switch (padded_states(N)) {
+        case 4: return F<T, 4>::run(p...);
+        case 8: return F<T, 8>::run(p...);
+        case 16: return F<T, 16>::run(p...);
+        case 32: return F<T, 32>::run(p...);
+        default: return F<T, 64>::run(p...);
+    }
+}
+template <typename T, int NP> struct FwdRun {
+    static janus_status run(const ScanArgs& a, const int32_t* lengths, hipStream_t st) {
+        return scan_fwd_run<T, NP>(a, lengths, st);
+    }
+};
+template <typename T, int NP> struct BwdRun {
+    static janus_status run(const ScanArgs& a, const int32_t* lengths, float* dA, float* dD, float* dtb, hipStream_t st) {
+        return scan_bwd_run<T, NP>(a, lengths, dA, dD, dtb, st);
+    }
+};
+template <typename T, int NP> struct StepRun {
+    static janus_status run(const ScanArgs& a, const int32_t* slots, int32_t n_slots, float* state, hipStream_t st) {
+        constexpr int QL = NP / 4;
+        const dim3 grid((int64_t(a.D) * QL + 255) / 256, a.B);
+        if (a.N % 4 == 0 && aligned(state, 16) && aligned(a.A, 16))
+            hipLaunchKernelGGL((scan_step_kernel<T, QL, true>), grid, dim3(256), 0, st, a, slots, n_slots, state);
+        else
+            hipLaunchKernelGGL((scan_step_kernel<T, QL, false>), grid, dim3(256), 0, st, a, slots, n_slots, state);
+        JANUS_LAUNCH_CHECK();
+        return JANUS_OK;
+    }
+};
+
+}  // namespace
+}  // namespace janus
+
+using namespace janus;
+
+extern "C" size_t janus_selective_scan_workspace_bytes(const janus_scan_desc* d) {
+    if (!scan_desc_ok(d) || !scan_supported(d)) return 0;
+    ScanArgs a = scan_geometry(d);
+    return scan_carve(a, d->flags & JANUS_SCAN_KEEP, nullptr);
+}
+
+extern "C" janus_status janus_selective_scan_fwd(const janus_scan_desc* d, const void* x, const void* dt,
+                                                 const float* A, const void* Bm, const void* Cm, const float* Dskip,
+                                                 const void* z, const float* dt_bias, const int32_t* lengths,
+                                                 const float* h0, void* y, float* hT, void* ws, size_t ws_bytes,
+                                                 void* stream) {
+    janus_status e = scan_check(d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, y, d && d->T > 0);
+    if (e != JANUS_OK) return e;
+    const bool keep = d->flags & JANUS_SCAN_KEEP;
+    if (!aligned(h0, 4) || !aligned(hT, 4) || (keep && hT && hT == h0)) return JANUS_ERR_INVALID_ARG;
+    if ((e = check_lengths(d->B, d->T, lengths)) != JANUS_OK) return e;
+    ScanArgs a = scan_geometry(d);
+    const size_t need = scan_carve(a, keep, ws);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 256))) return JANUS_ERR_WORKSPACE;
+    scan_inputs(a, x, dt, A, Bm, Cm, Dskip, z, dt_bias);
+    a.h0 = h0, a.y = y, a.hT = hT;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return d->dtype == JANUS_BF16 ? with_states<FwdRun, bf16_t>(a.N, a, lengths, st)
+                                  : with_states<FwdRun, float>(a.N, a, lengths, st);
+}
+
+extern "C" janus_status janus_selective_scan_bwd(const janus_scan_desc* d, const void* x, const void* dt,
+                                                 const float* A, const void* Bm, const void* Cm, const float* Dskip,
+                                                 const void* z, const float* dt_bias, const int32_t* lengths,
+                                                 const float* h0, const void* dy, const float* dhT, void* dx,
+                                                 void* ddt, float* dA, void* dBm, void* dCm, float* dDskip, void* dz,
+                                                 float* ddt_bias, float* dh0, void* ws, size_t ws_bytes,
+                                                 void* stream) {
+    const bool rows = d && d->T > 0;
+    janus_status e = scan_check(d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, dy, rows);
+    if (e != JANUS_OK) return e;
+    if (!(d->flags & JANUS_SCAN_KEEP) || !dA || (rows && (!dx || !ddt || !dBm || !dCm || (z && !dz))))
+        return JANUS_ERR_INVALID_ARG;
+    const size_t es = dtype_size(d->dtype);
+    for (const void* p : {static_cast<const void*>(dx), static_cast<const void*>(ddt), static_cast<const void*>(dBm),
+                          static_cast<const void*>(dCm), static_cast<const void*>(dz)}) {
+        if (!aligned(p, es)) return JANUS_ERR_INVALID_ARG;
+        for (const void* q : {x, dt, Bm, Cm, z, dy})
+            if (p && p == q) return JANUS_ERR_INVALID_ARG;
+    }
+    for (const float* p : {h0, dhT, static_cast<const float*>(dA), static_cast<const float*>(dDskip),
+                           static_cast<const float*>(ddt_bias), static_cast<const float*>(dh0)})
+        if (!aligned(p, 4)) return JANUS_ERR_INVALID_ARG;
+    if ((e = check_lengths(d->B, d->T, lengths)) != JANUS_OK) return e;
+    ScanArgs a = scan_geometry(d);
+    const size_t need = scan_carve(a, true, ws);
+    if (!ws || ws_bytes < need || !aligned(ws, 256)) return JANUS_ERR_WORKSPACE;
+    scan_inputs(a, x, dt, A, Bm, Cm, Dskip, z, dt_bias);
+    a.h0 = h0, a.dy = dy, a.dhT = dhT, a.dx = dx, a.ddt = ddt, a.dz = dz, a.dBm = dBm, a.dCm = dCm, a.dh0 = dh0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return d->dtype == JANUS_BF16 ? with_states<BwdRun, bf16_t>(a.N, a, lengths, dA, dDskip, ddt_bias, st)
+                                  : with_states<BwdRun, float>(a.N, a, lengths, dA, dDskip, ddt_bias, st);
+}
+
+extern "C" janus_status janus_selective_scan_step(const janus_scan_desc* d, const void* x, const void* dt,
+                                                  const float* A, const void* Bm, const void* Cm, const float* Dskip,
+                                                  const void* z, const float* dt_bias, const int32_t* slots,
+                                                  int32_t n_slots, float* state, void* y, void* stream) {
+    janus_status e = scan_check(d, x, dt, A, Bm, Cm, Dskip, z, dt_bias, y, true);
+    if (e != JANUS_OK) return e;
+    if (!state || n_slots < 1 || (!slots && n_slots < d->B) || !aligned(slots, 4) || !aligned(state, 4))
+        return JANUS_ERR_INVALID_ARG;
+    if (d->B > 65535) return JANUS_ERR_UNSUPPORTED;
+    ScanArgs a = scan_geometry(d);
+    scan_inputs(a, x, dt, A, Bm, Cm, Dskip, z, dt_bias);
+    a.y = y;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    TraceScope trace("scan_step", 7.0 * a.B * a.D * a.N, 8.0 * a.B * a.D * a.N, st);
+    return d->dtype == JANUS_BF16 ? with_states<StepRun, bf16_t>(a.N, a, slots, n_slots, state, st)
+                                  : with_states<StepRun, float>(a.N, a, slots, n_slots, state, st);
+}

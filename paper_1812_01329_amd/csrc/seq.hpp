@@ -1,0 +1,86 @@
+// What the convolution and the scan over variable-length sequences share:
+// argument checks, lengths passed to kernels by value, and loads and stores of
+// a few channels at once.
+#pragma once
+
+#include <algorithm>
+
+#include "device.hpp"
+#include "runtime.hpp"
+
+namespace janus {
+
+// The lengths of up to kSlice sequences as a kernel argument: no upload, no
+// device buffer, and a captured launch keeps its own copy.  Larger batches
+// take one launch per slice.
+constexpr int kSlice = 256;
+struct SeqSlice {
+    int32_t b0;               // first sequence of the slice
+    int32_t len[kSlice];
+};
+
+inline janus_status check_lengths(int32_t B, int32_t T, const int32_t* lengths) {
+    if (lengths)
+        for (int32_t b = 0; b < B; ++b)
+            if (lengths[b] < 0 || lengths[b] > T) return JANUS_ERR_LENGTH;
+    return JANUS_OK;
+}
+
+// Sequences [b0, b0 + kSlice) of the batch; returns how many there are.
+inline int fill_slice(SeqSlice& s, int32_t b0, int32_t B, int32_t T, const int32_t* lengths) {
+    const int n = std::min(kSlice, B - b0);
+    s.b0 = b0;
+    for (int i = 0; i < n; ++i) s.len[i] = lengths ? lengths[b0 + i] : T;
+    return n;
+}
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// VEC consecutive channels in one access (the pointer is aligned to it)
+template <typename T, int VEC> struct Chan;
+template <> struct Chan<float, 1> {
+    float v;
+    __device__ __forceinline__ void load(const float* p) { v = *p; }
+    __device__ __forceinline__ void get(float* f) const { f[0] = v; }
+    __device__ __forceinline__ static void store(float* p, const float* f) { *p = f[0]; }
+};
+template <> struct Chan<float, 4> {
+    float4 v;
+    __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+    __device__ __forceinline__ void get(float* f) const { f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w; }
+    __device__ __forceinline__ static void store(float* p, const float* f) {
+        *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    }
+};
+template <> struct Chan<bf16_t, 1> {
+    bf16_t v;
+    __device__ __forceinline__ void load(const bf16_t* p) { v = *p; }
+    __device__ __forceinline__ void get(float* f) const { f[0] = bf2f(v); }
+    __device__ __forceinline__ static void store(bf16_t* p, const float* f) { *p = f2bf(f[0]); }
+};
+// two bf16 of one word, and back
+__device__ __forceinline__ float lo2f(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float hi2f(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) { return uint32_t(f2bf(a)) | (uint32_t(f2bf(b)) << 16); }
+template <> struct Chan<bf16_t, 2> {
+    uint32_t v;
+    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const uint32_t*>(p); }
+    __device__ __forceinline__ void get(float* f) const { f[0] = lo2f(v), f[1] = hi2f(v); }
+    __device__ __forceinline__ static void store(bf16_t* p, const float* f) {
+        *reinterpret_cast<uint32_t*>(p) = pack2(f[0], f[1]);
+    }
+};
+template <> struct Chan<bf16_t, 8> {
+    uint4 v;
+    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void get(float* f) const {
+        f[0] = lo2f(v.x), f[1] = hi2f(v.x), f[2] = lo2f(v.y), f[3] = hi2f(v.y);
+        f[4] = lo2f(v.z), f[5] = hi2f(v.z), f[6] = lo2f(v.w), f[7] = hi2f(v.w);
+    }
+    __device__ __forceinline__ static void store(bf16_t* p, const float* f) {
+        *reinterpret_cast<uint4*>(p) =
+            make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+    }
+};
+
+}  // namespace janus

@@ -23,6 +23,8 @@ OK, ERR_INVALID_ARG, ERR_LENGTH, ERR_TREE, ERR_TOKEN, ERR_WORKSPACE, ERR_UNSUPPO
 F32, BF16 = 0, 1
 EMBED_FWD, XENT_FWD_BWD, EMBED_BWD = 0, 1, 2
 LOSS_SUMSQ, LOSS_MEAN = 0, 1
+CONV_LINEAR, CONV_SILU = 0, 1
+SCAN_SOFTPLUS, SCAN_KEEP = 1, 2
 
 EXPORTS = [
     "janus_lstm_workspace_bytes", "janus_lstm_seq_fwd", "janus_lstm_seq_bwd", "janus_lstm_device_report",
@@ -35,6 +37,9 @@ EXPORTS = [
     "janus_lstm_state_carry",
     "janus_treernn_workspace_bytes", "janus_treernn_fwd", "janus_treernn_bwd", "janus_treernn_device_report",
     "janus_childsum_workspace_bytes", "janus_childsum_fwd", "janus_childsum_bwd", "janus_childsum_device_report",
+    "janus_causal_conv_workspace_bytes", "janus_causal_conv_fwd", "janus_causal_conv_bwd", "janus_causal_conv_step",
+    "janus_selective_scan_workspace_bytes", "janus_selective_scan_fwd", "janus_selective_scan_bwd",
+    "janus_selective_scan_step", "janus_policy_workspace_bytes", "janus_policy_loss",
 ]
 
 
@@ -86,6 +91,22 @@ class MseDesc(C.Structure):
 
 class SgdDesc(C.Structure):
     _fields_ = [("n", C.c_int32), ("dtype", C.c_int), ("lr", C.c_float), ("max_norm", C.c_float)]
+
+
+class ConvDesc(C.Structure):
+    _fields_ = [("D", C.c_int32), ("K", C.c_int32), ("B", C.c_int32), ("T", C.c_int32), ("dtype", C.c_int),
+                ("act", C.c_int), ("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
+class ScanDesc(C.Structure):
+    _fields_ = [("D", C.c_int32), ("N", C.c_int32), ("G", C.c_int32), ("B", C.c_int32), ("T", C.c_int32),
+                ("dtype", C.c_int), ("flags", C.c_int32), ("ldx", C.c_int64), ("ldt", C.c_int64),
+                ("ldb", C.c_int64), ("ldc", C.c_int64), ("ldz", C.c_int64), ("ldy", C.c_int64)]
+
+
+class PolicyDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int), ("ld", C.c_int64),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float), ("ent_coef", C.c_float)]
 
 
 _lib = None
@@ -153,6 +174,20 @@ def lib():
         L.janus_mse_workspace_bytes.argtypes = [C.POINTER(MseDesc)]
         L.janus_linear_mse.argtypes = [C.POINTER(MseDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.janus_loss_reduce.argtypes = [C.c_int, vp, i64, vp, vp, vp]
+        L.janus_causal_conv_workspace_bytes.restype = sz
+        L.janus_causal_conv_workspace_bytes.argtypes = [C.POINTER(ConvDesc)]
+        L.janus_causal_conv_fwd.argtypes = [C.POINTER(ConvDesc), vp, pi32, vp, vp, vp, vp, vp, vp]
+        L.janus_causal_conv_bwd.argtypes = [C.POINTER(ConvDesc), vp, pi32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
+                                            vp]
+        L.janus_causal_conv_step.argtypes = [C.POINTER(ConvDesc), vp, vp, vp, vp, i32, vp, vp, vp]
+        L.janus_selective_scan_workspace_bytes.restype = sz
+        L.janus_selective_scan_workspace_bytes.argtypes = [C.POINTER(ScanDesc)]
+        L.janus_selective_scan_fwd.argtypes = [C.POINTER(ScanDesc)] + [vp] * 8 + [pi32] + [vp] * 4 + [sz, vp]
+        L.janus_selective_scan_bwd.argtypes = [C.POINTER(ScanDesc)] + [vp] * 8 + [pi32] + [vp] * 13 + [sz, vp]
+        L.janus_selective_scan_step.argtypes = [C.POINTER(ScanDesc)] + [vp] * 9 + [i32, vp, vp, vp]
+        L.janus_policy_workspace_bytes.restype = sz
+        L.janus_policy_workspace_bytes.argtypes = [C.POINTER(PolicyDesc)]
+        L.janus_policy_loss.argtypes = [C.POINTER(PolicyDesc)] + [vp] * 11 + [sz, vp]
         L.janus_trace_begin.argtypes = []
         L.janus_trace_end.argtypes = [C.POINTER(TraceStat), i32, C.POINTER(C.c_int32)]
         for name in EXPORTS:
@@ -417,6 +452,83 @@ def janus_lstm_state_carry(desc: LstmDesc, B_prev: int, hT, cT, h0, c0, stream=N
     the previous one (B_prev rows)."""
     st = lib().janus_lstm_state_carry(C.byref(desc), int(B_prev), _p(hT), _p(cT), _p(h0), _p(c0), _stream(stream))
     _check(st, "janus_lstm_state_carry")
+
+
+# ---------------------------------------------------------------- convolution and scan
+def janus_causal_conv_workspace_bytes(desc: ConvDesc) -> int:
+    return int(lib().janus_causal_conv_workspace_bytes(C.byref(desc)))
+
+
+def janus_causal_conv_fwd(desc: ConvDesc, x, lengths, w, bias, s0, y, sT=None, stream=None):
+    lens = _i32(lengths)
+    st = lib().janus_causal_conv_fwd(C.byref(desc), _p(x), _i32p(lens), _p(w), _p(bias), _p(s0), _p(y), _p(sT),
+                                     _stream(stream))
+    _check(st, "janus_causal_conv_fwd")
+
+
+def janus_causal_conv_bwd(desc: ConvDesc, x, lengths, w, bias, s0, dy, dsT, dx, dw, dbias, ds0, ws, stream=None):
+    lens = _i32(lengths)
+    st = lib().janus_causal_conv_bwd(C.byref(desc), _p(x), _i32p(lens), _p(w), _p(bias), _p(s0), _p(dy), _p(dsT),
+                                     _p(dx), _p(dw), _p(dbias), _p(ds0), _p(ws), ws.numel() * ws.element_size(),
+                                     _stream(stream))
+    _check(st, "janus_causal_conv_bwd")
+
+
+def janus_causal_conv_step(desc: ConvDesc, x, w, bias, state, y, slots=None, stream=None):
+    """One token of desc.B sequences; ``state`` [n_slots, K-1, D] is updated
+    in place, ``slots`` a device int32 tensor (None: row b has slot b)."""
+    n_slots = desc.B if state is None else state.shape[0]
+    st = lib().janus_causal_conv_step(C.byref(desc), _p(x), _p(w), _p(bias), _p(slots), n_slots, _p(state), _p(y),
+                                      _stream(stream))
+    _check(st, "janus_causal_conv_step")
+
+
+def janus_selective_scan_workspace_bytes(desc: ScanDesc) -> int:
+    return int(lib().janus_selective_scan_workspace_bytes(C.byref(desc)))
+
+
+def janus_selective_scan_fwd(desc: ScanDesc, x, dt, A, Bm, Cm, lengths, y, ws=None, Dskip=None, z=None, dt_bias=None,
+                             h0=None, hT=None, stream=None):
+    lens = _i32(lengths)
+    st = lib().janus_selective_scan_fwd(C.byref(desc), _p(x), _p(dt), _p(A), _p(Bm), _p(Cm), _p(Dskip), _p(z),
+                                        _p(dt_bias), _i32p(lens), _p(h0), _p(y), _p(hT), _p(ws),
+                                        0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "janus_selective_scan_fwd")
+
+
+def janus_selective_scan_bwd(desc: ScanDesc, x, dt, A, Bm, Cm, lengths, dy, ws, dx, ddt, dA, dBm, dCm, Dskip=None,
+                             z=None, dt_bias=None, h0=None, dhT=None, dDskip=None, dz=None, ddt_bias=None, dh0=None,
+                             stream=None):
+    lens = _i32(lengths)
+    st = lib().janus_selective_scan_bwd(C.byref(desc), _p(x), _p(dt), _p(A), _p(Bm), _p(Cm), _p(Dskip), _p(z),
+                                        _p(dt_bias), _i32p(lens), _p(h0), _p(dy), _p(dhT), _p(dx), _p(ddt), _p(dA),
+                                        _p(dBm), _p(dCm), _p(dDskip), _p(dz), _p(ddt_bias), _p(dh0), _p(ws),
+                                        ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "janus_selective_scan_bwd")
+
+
+def janus_selective_scan_step(desc: ScanDesc, x, dt, A, Bm, Cm, state, y, Dskip=None, z=None, dt_bias=None,
+                              slots=None, stream=None):
+    """One token of desc.B sequences; ``state`` [n_slots, D, N] float32 is
+    updated in place, ``slots`` as in janus_causal_conv_step."""
+    st = lib().janus_selective_scan_step(C.byref(desc), _p(x), _p(dt), _p(A), _p(Bm), _p(Cm), _p(Dskip), _p(z),
+                                         _p(dt_bias), _p(slots), state.shape[0], _p(state), _p(y), _stream(stream))
+    _check(st, "janus_selective_scan_step")
+
+
+# ---------------------------------------------------------------- policy loss
+def janus_policy_workspace_bytes(desc: PolicyDesc) -> int:
+    return int(lib().janus_policy_workspace_bytes(C.byref(desc)))
+
+
+def janus_policy_loss(desc: PolicyDesc, logits, actions, old_logp=None, adv=None, ref_logp=None, weights=None,
+                      dlogits=None, logp=None, entropy=None, stats=None, ws=None, stream=None):
+    """Loss statistics and logits' gradient, or (without old_logp, adv and
+    dlogits) only the rows' log-probabilities and entropies."""
+    st = lib().janus_policy_loss(C.byref(desc), _p(logits), _p(actions), _p(old_logp), _p(adv), _p(ref_logp),
+                                 _p(weights), _p(dlogits), _p(logp), _p(entropy), _p(stats), _p(ws),
+                                 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "janus_policy_loss")
 
 
 # ---------------------------------------------------------------- update
