@@ -31,19 +31,32 @@ struct ConvArgs {
     void* dx;
     float* ds0;
     float* part;        // [parts, K + 1, D] sums of dw and dbias, or NULL
-    bool silu;
+    bool silu, w16;     // w16: w is 16-byte aligned
 };
 
-// the value `back` steps before time 0 is row K - 1 - back of the state
+// The taps and biases of a lane's channels; in 16-byte loads where the lanes'
+// parts of w [D, K] are whole ones of those (each tap alone is K loads a channel).
 template <typename T, int K, int VEC>
 __device__ __forceinline__ void load_taps(const ConvArgs& a, int d, float (&w)[K][VEC], float (&bias)[VEC]) {
-    const T* wp = static_cast<const T*>(a.w);
+    constexpr int N = K * VEC, PER = 16 / sizeof(T);
+    const T* wp = static_cast<const T*>(a.w) + int64_t(d) * K;
     const T* bp = static_cast<const T*>(a.bias);
+    T raw[N];
+    if (N % PER == 0 && a.w16) {
+#pragma unroll
+        for (int i = 0; i < N / PER; ++i) {
+            const uint4 v = reinterpret_cast<const uint4*>(wp)[i];
+            __builtin_memcpy(raw + i * PER, &v, 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) raw[i] = wp[i];
+    }
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
         bias[v] = bp ? to_f(bp[d + v]) : 0.f;
 #pragma unroll
-        for (int k = 0; k < K; ++k) w[k][v] = to_f(wp[int64_t(d + v) * K + k]);
+        for (int k = 0; k < K; ++k) w[k][v] = to_f(raw[v * K + k]);
     }
 }
 
@@ -118,131 +131,177 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a, SeqSlice s) {
     }
 }
 
-// A lane walks over items (sequence, segment) blockIdx.y, + gridDim.y, ... of
-// the slice and keeps the sums of dw and dbias in registers.  At time u it has
-// g_u and so dx_{u-K+1}; an item reads K - 1 rows past its end for the last
-// ones, and the first item of a sequence starts K - 1 steps early in dx: the
-// gradient of the carried state.
-template <typename T, int K, int VEC>
-__global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a, SeqSlice s, int items, int part0) {
-    const int d = (blockIdx.x * blockDim.x + threadIdx.x) * VEC;
-    if (d >= a.D) return;
-    float w[K][VEC], bias[VEC], dw[K][VEC], db[VEC];
-    load_taps<T, K, VEC>(a, d, w, bias);
+// What a lane keeps between the time steps of an item
+template <int K, int VEC>
+struct ConvWin {
+    float x[K][VEC], g[K][VEC];   // [j]: of time u - K + 1 + j
+    __device__ __forceinline__ void shift() {
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-        db[v] = 0.f;
+        for (int k = 0; k + 1 < K; ++k)
 #pragma unroll
-        for (int k = 0; k < K; ++k) dw[k][v] = 0.f;
+            for (int v = 0; v < VEC; ++v) x[k][v] = x[k + 1][v], g[k][v] = g[k + 1][v];
     }
+};
+
+// A lane walks over items (sequence, segment) of the slice and keeps the sums of
+// dw and dbias in registers.  At time u it has g_u and so dx_{u-K+1}; an item
+// reads K - 1 rows past its end for the last ones, and the first item of a
+// sequence starts K - 1 steps early in dx: the gradient of the carried state.
+// A workgroup is `groups` rows of lanes, each with its own items; their sums
+// are added in LDS, which leaves a part a workgroup to write.
+template <typename T, int K, int VEC>
+__global__ __launch_bounds__(512) void conv_bwd_kernel(ConvArgs a, SeqSlice s, int items, int part0, int lanes,
+                                                       int groups) {
+    extern __shared__ float red[];   // [groups - 1][lanes * VEC]
+    const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
+    const int d = (blockIdx.x * lanes + lane) * VEC;
+    const bool on = d < a.D && group < groups;
+    float w[K][VEC], bias[VEC], dw[K + 1][VEC];   // dw[K]: dbias
+#pragma unroll
+    for (int v = 0; v < VEC; ++v)
+#pragma unroll
+        for (int k = 0; k <= K; ++k) dw[k][v] = 0.f;
+    if (on) load_taps<T, K, VEC>(a, d, w, bias);
     const int64_t sx = a.B * a.ldx, sy = a.B * a.ldy;
-    for (int item = blockIdx.y; item < items; item += gridDim.y) {
+    for (int item = blockIdx.y * groups + group; on && item < items; item += gridDim.y * groups) {
         const int bs = item / a.nseg, seg = item - bs * a.nseg;
         const int len = s.len[bs], b = s.b0 + bs;
         const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg);
         const T* xp = static_cast<const T*>(a.x) + b * a.ldx + d;
         const T* gp = static_cast<const T*>(a.dy) + b * a.ldy + d;
         T* dxp = a.dx ? static_cast<T*>(a.dx) + b * a.ldx + d : nullptr;
-        float win[K][VEC], g[K][VEC];   // g[j]: g of time u - K + 1 + j
+        ConvWin<K, VEC> win;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) g[k][v] = win[k][v] = 0.f;
+            for (int v = 0; v < VEC; ++v) win.x[k][v] = win.g[k][v] = 0.f;
         if (t0 < len) {
 #pragma unroll
-            for (int k = 0; k < K - 1; ++k) load_input<T, K, VEC>(a, b, t0 - K + 1 + k, d, win[k]);
+            for (int k = 0; k < K - 1; ++k) load_input<T, K, VEC>(a, b, t0 - K + 1 + k, d, win.x[k]);
         }
+        // g_u from row u, and its part of the sums (the rows past the segment are the next item's)
+        auto take = [&](const Chan<T, VEC>& rx, const Chan<T, VEC>& rg, bool sum) {
+            rx.get(win.x[K - 1]);
+            rg.get(win.g[K - 1]);
+            if (a.silu) {
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) {
+                    float p = bias[v];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) p = fmaf(w[k][v], win.x[k][v], p);
+                    const float q = sigmoidf_(p);
+                    win.g[K - 1][v] *= q * (1.f + p * (1.f - q));
+                }
+            }
+            if (sum) {
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) {
+                    dw[K][v] += win.g[K - 1][v];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) dw[k][v] = fmaf(win.g[K - 1][v], win.x[k][v], dw[k][v]);
+                }
+            }
+        };
+        auto input_grad = [&](float (&dx)[VEC]) {
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                dx[v] = 0.f;
+#pragma unroll
+                for (int j = 0; j < K; ++j) dx[v] = fmaf(w[K - 1 - j][v], win.g[j][v], dx[v]);
+            }
+        };
+        // one step at the edges of a segment or a sequence
+        auto edge = [&](const Chan<T, VEC>& rx, const Chan<T, VEC>& rg, int u) {
+            if (u < len) {
+                take(rx, rg, u < t1);
+            } else {
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) win.g[K - 1][v] = 0.f;
+            }
+            const int t = u - (K - 1);
+            if (t >= t0 || seg == 0) {
+                float dx[VEC] = {};
+                if (t < len) {
+                    input_grad(dx);
+                    const int i = t - (len - (K - 1));   // row of the final state
+                    if (a.dsT && i >= 0) {
+#pragma unroll
+                        for (int v = 0; v < VEC; ++v) dx[v] += a.dsT[(int64_t(b) * (K - 1) + i) * a.D + d + v];
+                    }
+                }
+                if (t >= 0) {
+                    if (dxp) Chan<T, VEC>::store(dxp + t * sx, dx);
+                } else if (a.ds0) {
+#pragma unroll
+                    for (int v = 0; v < VEC; ++v)
+                        a.ds0[(int64_t(b) * (K - 1) + (K - 1 + t)) * a.D + d + v] = dx[v];
+                }
+            }
+            win.shift();
+        };
         constexpr int U = 4;
-        for (int u0 = t0; u0 < t1 + K - 1; u0 += U) {
-            Chan<T, VEC> rx[U], rg[U];
+        const int ue = t1 + K - 1, ul = min(ue, len);
+        Chan<T, VEC> rx[U], rg[U], nx[U], ng[U];   // rows [u, u + U) and the U after them, on their way
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (t0 + i < ul) nx[i].load(xp + (t0 + i) * sx), ng[i].load(gp + (t0 + i) * sy);
+        for (int u = t0; u < ue; u += U) {
+#pragma unroll
+            for (int i = 0; i < U; ++i) rx[i] = nx[i], rg[i] = ng[i];
 #pragma unroll
             for (int i = 0; i < U; ++i)
-                if (u0 + i < min(t1 + K - 1, len)) {
-                    rx[i].load(xp + (u0 + i) * sx);
-                    rg[i].load(gp + (u0 + i) * sy);
-                }
+                if (u + U + i < ul) nx[i].load(xp + (u + U + i) * sx), ng[i].load(gp + (u + U + i) * sy);
+            if (u >= t0 + K - 1 && u + U <= min(t1, len)) {   // their dx is this item's and no part of the final state
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int u = u0 + i;
-                if (u >= t1 + K - 1) break;
-                if (u < len) {
-                    rx[i].get(win[K - 1]);
-                    rg[i].get(g[K - 1]);
-                    if (a.silu) {
-#pragma unroll
-                        for (int v = 0; v < VEC; ++v) {
-                            float p = bias[v];
-#pragma unroll
-                            for (int k = 0; k < K; ++k) p = fmaf(w[k][v], win[k][v], p);
-                            const float q = sigmoidf_(p);
-                            g[K - 1][v] *= q * (1.f + p * (1.f - q));
-                        }
-                    }
-                    if (u < t1) {
-#pragma unroll
-                        for (int v = 0; v < VEC; ++v) {
-                            db[v] += g[K - 1][v];
-#pragma unroll
-                            for (int k = 0; k < K; ++k) dw[k][v] = fmaf(g[K - 1][v], win[k][v], dw[k][v]);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int v = 0; v < VEC; ++v) g[K - 1][v] = 0.f;
-                }
-                const int t = u - (K - 1);
-                if (t >= t0 || seg == 0) {
+                for (int i = 0; i < U; ++i) {
+                    take(rx[i], rg[i], true);
                     float dx[VEC];
-                    if (t < len) {
-#pragma unroll
-                        for (int v = 0; v < VEC; ++v) {
-                            dx[v] = 0.f;
-#pragma unroll
-                            for (int j = 0; j < K; ++j) dx[v] = fmaf(w[K - 1 - j][v], g[j][v], dx[v]);
-                        }
-                        const int i_s = t - (len - (K - 1));
-                        if (a.dsT && i_s >= 0) {
-#pragma unroll
-                            for (int v = 0; v < VEC; ++v)
-                                dx[v] += a.dsT[(int64_t(b) * (K - 1) + i_s) * a.D + d + v];
-                        }
-                    } else {
-#pragma unroll
-                        for (int v = 0; v < VEC; ++v) dx[v] = 0.f;
-                    }
-                    if (t >= 0) {
-                        if (dxp) Chan<T, VEC>::store(dxp + t * sx, dx);
-                    } else if (a.ds0) {
-#pragma unroll
-                        for (int v = 0; v < VEC; ++v)
-                            a.ds0[(int64_t(b) * (K - 1) + (K - 1 + t)) * a.D + d + v] = dx[v];
-                    }
+                    input_grad(dx);
+                    if (dxp) Chan<T, VEC>::store(dxp + (u + i - (K - 1)) * sx, dx);
+                    win.shift();
                 }
+            } else {
 #pragma unroll
-                for (int k = 0; k + 1 < K; ++k)
-#pragma unroll
-                    for (int v = 0; v < VEC; ++v) win[k][v] = win[k + 1][v], g[k][v] = g[k + 1][v];
+                for (int i = 0; i < U; ++i)
+                    if (u + i < ue) edge(rx[i], rg[i], u + i);
             }
         }
     }
-    if (a.part) {
-        float* p = a.part + int64_t(part0 + blockIdx.y) * (K + 1) * a.D + d;
+    if (!a.part) return;
+    float* p = a.part + int64_t(part0 + blockIdx.y) * (K + 1) * a.D;
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
+    for (int k = 0; k <= K; ++k) {
+        if (group > 0 && group < groups) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) p[int64_t(k) * a.D + v] = dw[k][v];
-            p[int64_t(K) * a.D + v] = db[v];
+            for (int v = 0; v < VEC; ++v) red[(group - 1) * lanes * VEC + v * lanes + lane] = dw[k][v];
         }
+        __syncthreads();
+        if (group == 0 && on) {
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                float f = dw[k][v];
+                for (int g = 0; g < groups - 1; ++g) f += red[g * lanes * VEC + v * lanes + lane];
+                p[int64_t(k) * a.D + d + v] = f;
+            }
+        }
+        __syncthreads();
     }
 }
 
-// dw [D, K] and dbias [D] from the parts, summed in their order
-__global__ __launch_bounds__(256) void conv_param_kernel(const float* part, int parts, int D, int K, float* dw,
-                                                         float* dbias) {
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;   // k * D + d
-    if (i >= (K + 1) * D) return;
+// dw [D, K] and dbias [D] from the parts: 64 values a workgroup, each wave sums
+// every 16th part, then the waves' sums in their order.
+__global__ __launch_bounds__(1024) void conv_param_kernel(const float* part, int parts, int D, int K, float* dw,
+                                                          float* dbias) {
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (K + 1) * D;
+    const int i = blockIdx.x * 64 + lane;   // k * D + d
     float s = 0.f;
-    for (int p = 0; p < parts; ++p) s += part[int64_t(p) * (K + 1) * D + i];
+    if (i < n)
+        for (int p = wave; p < parts; p += 16) s += part[int64_t(p) * n + i];
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || i >= n) return;
+    for (int w = 1; w < 16; ++w) s += red[w][lane];
     const int k = i / D, d = i - k * D;
     if (k < K) {
         if (dw) dw[int64_t(d) * K + k] = s;
@@ -311,16 +370,21 @@ ConvArgs conv_args(const janus_conv_desc* d, const void* x, const void* w, const
     a.ldy = d->ldy ? d->ldy : d->D;
     a.x = x, a.w = w, a.bias = bias, a.s0 = s0;
     a.silu = d->act == JANUS_CONV_SILU;
+    a.w16 = aligned(w, 16);
     return a;
 }
 
-// Channels per lane: the widest access that every row of every operand is
-// aligned to (16 bytes, 4 bytes for bf16 of an even width, else one element).
+// Channels per lane: 4, or 2 for bf16, or 1: as many as every row of every
+// operand is aligned to and as leave a wave's lanes filled.  (8 bf16 channels
+// a lane take so many registers that fewer waves hide the loads' latency:
+// 25600 rows of 1024 channels, half of them past their ends, forward 28.8 us
+// with 8, 21.8 with 4, 23.2 with 2.)
 int conv_vec(const janus_conv_desc* d, const ConvArgs& a, std::initializer_list<const void*> ptrs) {
     const size_t es = dtype_size(d->dtype);
-    for (int bytes : {16, 4}) {
-        const int v = int(bytes / es);
-        bool ok = a.D % v == 0 && a.ldx % v == 0 && a.ldy % v == 0;
+    for (int v : {4, 2}) {
+        if (v == 2 && es == 4) continue;
+        const size_t bytes = v * es;
+        bool ok = a.D % v == 0 && a.D / v >= 64 && a.ldx % v == 0 && a.ldy % v == 0;
         for (const void* p : ptrs) ok = ok && aligned(p, bytes);
         if (ok) return v;
     }
@@ -346,7 +410,7 @@ void conv_dispatch(janus_dtype dt, int K, int vec, F f) {
         if (vec == 4) with_taps<float, 4>(K, f);
         else with_taps<float, 1>(K, f);
     } else {
-        if (vec == 8) with_taps<bf16_t, 8>(K, f);
+        if (vec == 4) with_taps<bf16_t, 4>(K, f);
         else if (vec == 2) with_taps<bf16_t, 2>(K, f);
         else with_taps<bf16_t, 1>(K, f);
     }
@@ -364,11 +428,12 @@ struct FwdLaunch {
 struct BwdLaunch {
     const ConvArgs& a;
     const SeqSlice& s;
-    int items, part0;
-    dim3 grid, block;
+    int items, part0, lanes, groups;
+    dim3 grid;
     hipStream_t st;
     template <typename T, int K, int VEC> void go() {
-        hipLaunchKernelGGL((conv_bwd_kernel<T, K, VEC>), grid, block, 0, st, a, s, items, part0);
+        hipLaunchKernelGGL((conv_bwd_kernel<T, K, VEC>), grid, dim3(lanes * groups),
+                           size_t(groups - 1) * lanes * VEC * sizeof(float), st, a, s, items, part0, lanes, groups);
     }
 };
 struct StepLaunch {
@@ -383,7 +448,7 @@ struct StepLaunch {
 };
 
 // Threads of a block of the channels, blocks along them, and how the time axis
-// is cut: segments of at least 32 steps, as many as it takes for 4096 waves.
+// is cut: segments of at least 16 steps, as many as it takes for 4096 waves.
 struct ConvShape {
     int threads, blocks;
 };
@@ -393,18 +458,19 @@ ConvShape conv_shape(ConvArgs& a, int vec) {
     c.threads = std::min(256, int(round_up(lanes, 64)));
     c.blocks = (lanes + c.threads - 1) / c.threads;
     const int64_t waves = int64_t(a.B) * ((lanes + 63) / 64);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(a.T / 32, 4096 / waves));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(a.T / 16, 4096 / waves));
     a.seg = std::max(1, int((a.T + want - 1) / want));
     a.nseg = std::max(1, (a.T + a.seg - 1) / a.seg);
     return c;
 }
 
-// parts of the sums of dw and dbias: blocks of one slice along the items
-constexpr int kConvParts = 64;
+// Parts of the sums of dw and dbias in one slice, at most: workgroups of 8 waves
+// along the items, for two waves a SIMD of 4 channels a lane and D up to 4096.
+int conv_parts(int32_t D) { return std::max(16, 256 / ((D + 4095) / 4096)); }
 int conv_slices(int32_t B) { return (B + kSlice - 1) / kSlice; }
 size_t conv_ws_bytes(const janus_conv_desc* d) {
     Carver c(nullptr);
-    c.take<float>(size_t(conv_slices(d->B)) * kConvParts * (d->K + 1) * d->D);
+    c.take<float>(size_t(conv_slices(d->B)) * conv_parts(d->D) * (d->K + 1) * d->D);
     return c.off;
 }
 
@@ -463,16 +529,17 @@ extern "C" janus_status janus_causal_conv_bwd(const janus_conv_desc* d, const vo
     for (int32_t b0 = 0; b0 < d->B; b0 += kSlice) {
         SeqSlice s;
         const int n = fill_slice(s, b0, d->B, d->T, lengths);
-        const int items = n * a.nseg, rows = a.part ? std::min(items, kConvParts) : std::min(items, 65535);
+        const int items = n * a.nseg, groups = std::min(512 / c.threads, items);
+        const int rows = std::min((items + groups - 1) / groups, conv_parts(d->D));
         TraceScope trace("conv_bwd", el / d->B * n * 6 * d->K, el / d->B * n * 3 * dtype_size(d->dtype), st);
-        conv_dispatch(d->dtype, d->K, vec, BwdLaunch{a, s, items, parts, dim3(c.blocks, rows), dim3(c.threads), st});
+        conv_dispatch(d->dtype, d->K, vec, BwdLaunch{a, s, items, parts, c.threads, groups, dim3(c.blocks, rows), st});
         JANUS_LAUNCH_CHECK();
         parts += rows;
     }
     if (a.part) {
         const int n = (d->K + 1) * d->D;
         TraceScope trace("conv_param", double(n) * parts, 4.0 * n * parts, st);
-        hipLaunchKernelGGL(conv_param_kernel, dim3((n + 255) / 256), dim3(256), 0, st, a.part, parts, d->D, d->K, dw,
+        hipLaunchKernelGGL(conv_param_kernel, dim3((n + 63) / 64), dim3(1024), 0, st, a.part, parts, d->D, d->K, dw,
                            dbias);
         JANUS_LAUNCH_CHECK();
     }

@@ -106,7 +106,7 @@ struct Row {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const int i = p * VEC + j;
-                r.set(j, i >= lo && i < hi ? base[i] : from_f<T>(-INFINITY));
+                r.set(j, i >= lo && i < hi ? base[i] : out_f<T>(-INFINITY));
             }
         }
         return r;
@@ -119,7 +119,7 @@ struct Row {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const int i = p * VEC + j;
-                if (i >= lo && i < hi) out[i] = from_f<T>(f[j]);
+                if (i >= lo && i < hi) out[i] = out_f<T>(f[j]);
             }
         }
     }
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a) {
                 x[i] = row.load(p);
             } else {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) x[i].set(j, from_f<T>(-INFINITY));
+                for (int j = 0; j < VEC; ++j) x[i].set(j, out_f<T>(-INFINITY));
             }
         }
 #pragma unroll

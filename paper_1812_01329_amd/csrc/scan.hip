@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
                         const float z = to_f(rz[i]);
                         y *= z * sigmoidf_(z);
                     }
-                    yp[t * sy] = from_f<T>(y);
+                    yp[t * sy] = out_f<T>(y);
                 }
             }
         }
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
         a.seg_e[(int64_t(seg) * a.B + b) * a.D + d] = esum;
         return;
     }
-    for (int t = max(t0, len); t < t1; ++t) yp[t * sy] = from_f<T>(0.f);
+    for (int t = max(t0, len); t < t1; ++t) yp[t * sy] = out_f<T>(0.f);
     if (a.hT && seg == a.nseg - 1) {
 #pragma unroll
         for (int n = 0; n < NP; ++n)
@@ -489,16 +489,16 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a, SeqSlice s
                 float dz = 0.f;
                 if (GATE) dz = sh[wave][GATE ? 5 : 0][k][own] * fmaf(dskip, ox, fold_rows(yr));
                 if (k < tn && live) {   // 0 past the sequence's end: e, u, gy, x are
-                    dxp[(tc + k) * sx] = from_f<T>(fmaf(ogy, dskip, oe * S));
-                    dtp[(tc + k) * st] = from_f<T>(ddt);
-                    if (GATE) dzp[(tc + k) * sz] = from_f<T>(dz);
+                    dxp[(tc + k) * sx] = out_f<T>(fmaf(ogy, dskip, oe * S));
+                    dtp[(tc + k) * st] = out_f<T>(ddt);
+                    if (GATE) dzp[(tc + k) * sz] = out_f<T>(dz);
                 }
             }
         } else if (live) {
             for (int k = 0; k < tn; ++k) {
-                dxp[(tc + k) * sx] = from_f<T>(0.f);
-                dtp[(tc + k) * st] = from_f<T>(0.f);
-                if (GATE) dzp[(tc + k) * sz] = from_f<T>(0.f);
+                dxp[(tc + k) * sx] = out_f<T>(0.f);
+                dtp[(tc + k) * st] = out_f<T>(0.f);
+                if (GATE) dzp[(tc + k) * sz] = out_f<T>(0.f);
             }
         }
         __syncthreads();
@@ -511,8 +511,8 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a, SeqSlice s
             if (a.bc_part) {
                 a.bc_part[((int64_t(blk) * a.T * a.B + row) * a.G + group) * 2 * NP + m] = v;
             } else if (n < a.N) {
-                if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = from_f<T>(v);
-                else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = from_f<T>(v);
+                if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = out_f<T>(v);
+                else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = out_f<T>(v);
             }
         }
     }
@@ -560,8 +560,8 @@ __global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a) {
     if (n >= a.N) return;
     float v = 0.f;
     for (int k = 0; k < a.blocks; ++k) v += a.bc_part[k * all + i];
-    if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = from_f<T>(v);
-    else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = from_f<T>(v);
+    if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = out_f<T>(v);
+    else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = out_f<T>(v);
 }
 
 // One token: QL lanes per channel with 4 states each.
@@ -574,7 +574,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, const int32_
     const int slot = slots ? slots[b] : b;
     T* yp = static_cast<T*>(a.y) + b * a.ldy + d;
     if (slot < 0 || slot >= n_slots) {
-        if (live && q == 0) *yp = from_f<T>(0.f);
+        if (live && q == 0) *yp = out_f<T>(0.f);
         return;
     }
     const int n0 = 4 * q, group = d / a.Dg;
@@ -622,7 +622,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, const int32_
             const float z = to_f(static_cast<const T*>(a.z)[b * a.ldz + d]);
             y *= z * sigmoidf_(z);
         }
-        *yp = from_f<T>(y);
+        *yp = out_f<T>(y);
     }
 }
 

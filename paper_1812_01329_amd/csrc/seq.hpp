@@ -36,6 +36,17 @@ inline int fill_slice(SeqSlice& s, int32_t b0, int32_t B, int32_t T, const int32
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
+// float -> bf16, round to nearest even (v_cvt_pk_bf16_f32)
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const f32x2_t v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+}
+template <typename T> __device__ __forceinline__ T out_f(float v);
+template <> __device__ __forceinline__ float out_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16_t out_f<bf16_t>(float v) { return __builtin_bit_cast(bf16_t, (__bf16)v); }
+
 // VEC consecutive channels in one access (the pointer is aligned to it)
 template <typename T, int VEC> struct Chan;
 template <> struct Chan<float, 1> {
@@ -56,18 +67,27 @@ template <> struct Chan<bf16_t, 1> {
     bf16_t v;
     __device__ __forceinline__ void load(const bf16_t* p) { v = *p; }
     __device__ __forceinline__ void get(float* f) const { f[0] = bf2f(v); }
-    __device__ __forceinline__ static void store(bf16_t* p, const float* f) { *p = f2bf(f[0]); }
+    __device__ __forceinline__ static void store(bf16_t* p, const float* f) { *p = out_f<bf16_t>(f[0]); }
 };
 // two bf16 of one word, and back
 __device__ __forceinline__ float lo2f(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float hi2f(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack2(float a, float b) { return uint32_t(f2bf(a)) | (uint32_t(f2bf(b)) << 16); }
 template <> struct Chan<bf16_t, 2> {
     uint32_t v;
     __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const uint32_t*>(p); }
     __device__ __forceinline__ void get(float* f) const { f[0] = lo2f(v), f[1] = hi2f(v); }
     __device__ __forceinline__ static void store(bf16_t* p, const float* f) {
         *reinterpret_cast<uint32_t*>(p) = pack2(f[0], f[1]);
+    }
+};
+template <> struct Chan<bf16_t, 4> {
+    uint2 v;
+    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const uint2*>(p); }
+    __device__ __forceinline__ void get(float* f) const {
+        f[0] = lo2f(v.x), f[1] = hi2f(v.x), f[2] = lo2f(v.y), f[3] = hi2f(v.y);
+    }
+    __device__ __forceinline__ static void store(bf16_t* p, const float* f) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1]), pack2(f[2], f[3]));
     }
 };
 template <> struct Chan<bf16_t, 8> {
