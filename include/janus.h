@@ -632,8 +632,9 @@ size_t janus_selective_scan_workspace_bytes(const janus_scan_desc* d);
  *  y        [T, B, D] dtype; not an input.
  * Errors: NULL d/A, NULL x/dt/Bm/Cm/y with T > 0, a non-positive D, N, G, B,
  * T < 0, D not a multiple of G, a stride below a row, a pointer not aligned to
- * its element -> INVALID_ARG; N > 64, a dtype or flag not listed ->
- * UNSUPPORTED; LENGTH; WORKSPACE.
+ * its element -> INVALID_ARG; N > 64, D > 2^22, B times a row stride of x, dt,
+ * z or y past 2^29 elements, a dtype or flag not listed -> UNSUPPORTED;
+ * LENGTH; WORKSPACE.
  */
 janus_status janus_selective_scan_fwd(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
                                       const void* Bm, const void* Cm, const float* Dskip, const void* z,

@@ -17,6 +17,8 @@
 // segment's state from a zero start, a small kernel chains them (the decay over
 // a segment is exp(A sum e)), and the second pass starts from the right state.
 // States, decays and every sum over states, time or channels are float32.
+#include <type_traits>
+
 #include "seq.hpp"
 
 namespace janus {
@@ -29,10 +31,18 @@ constexpr int kStage = 32;    // steps whose B and C rows lie in LDS at once
 // Steps between two kept states: the backward holds the states of one such
 // chunk in registers (128 floats a lane for 16 states and more).
 constexpr int chunk_steps(int NP) { return NP <= 8 ? 16 : 128 / NP; }
+#ifndef MW
+#define MW 2
+#endif
+#ifndef BW
+#define BW 4
+#endif
+constexpr int kBwdWaves = BW;
 
 struct ScanArgs {
     int32_t D, N, G, Dg, B, T;
     int32_t tiles, blocks;    // 64-channel tiles of a group, workgroups of a group
+    int32_t btiles, bblocks;  // the backward's 32-channel tiles, and workgroups
     int32_t seg, nseg;        // steps per segment (a multiple of kStage), segments
     int64_t ldx, ldt, ldb, ldc, ldz, ldy;
     const void *x, *dt, *Bm, *Cm, *z;
@@ -50,7 +60,7 @@ struct ScanArgs {
     float* seg_g;     // as seg_h, for G in reverse time
     float* dA_part;   // [nseg * B][D][N]
     float* dv_part;   // [nseg * B][2][D] sums of gy x and of ddt
-    float* bc_part;   // [blocks][T * B][G][2][NP], or NULL with one workgroup a group
+    float* bc_part;   // [bblocks][T * B][G][2][NP], or NULL with one workgroup a group
     bool softplus;
 };
 
@@ -65,6 +75,17 @@ __device__ __forceinline__ float softplus_(float v) {
     return fmaxf(v, 0.f) + l;
 }
 __device__ __forceinline__ float step_size(float v, bool softplus) { return softplus ? softplus_(v) : v; }
+
+// The same address in every lane, and known to the compiler as such: a load or
+// store then takes it from scalar registers and only the lane's offset (32 bits)
+// from a vector register.
+template <typename P>
+__device__ __forceinline__ P* uniform(P* p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(v >> 32));
+    return reinterpret_cast<P*>(uint64_t(hi) << 32 | lo);
+}
 
 // [seg or chunk][b][quarter][d][4]
 template <int NP>
@@ -296,9 +317,6 @@ __device__ __forceinline__ float fold32(float a, float b) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-// v[r] summed over the four 16-lane rows; row r keeps v[r]
-__device__ __forceinline__ float fold_rows(const float (&v)[4]) { return fold32(fold16(v[0], v[1]), fold16(v[2], v[3])); }
-
 // M values summed over the 16 lanes of a row.  Where there are values left to
 // share, each step leaves a lane with half of them (which half: a bit of the
 // lane's number); then it sums.  Lane l ends with values first(l) + [0, max(1, M / 16)).
@@ -338,129 +356,163 @@ struct RowFold {
     }
 };
 
-// Backward of one segment.  A wave's 64 channels lie 4 to a lane (lane l: channels
-// 4 (l % 16) + [0, 4)) and the states in four parts over the wave's 16-lane
-// rows, so the sums over channels that dB and dC need are mostly in-lane, and
-// the sums over states cost six operations for four channels.  fold_rows leaves
-// lane l with channel 4 (l % 16) + l / 16, for which it does the work per
-// channel (step size, gate, stores); values cross between the two layouts in LDS.
-// Chunks go backwards; the states inside one are formed again from its start.
+// What was read from LDS before is read again after: keeps the compiler from
+// holding a chunk's decays in registers beside its states.
+__device__ __forceinline__ void forget_lds() { asm volatile("" ::: "memory"); }
+
+// A row (t, b) of an operand and the one after it, t + 1: a uniform address, and
+// the 32-bit byte offset of the lane's channel in one of the two.
+struct RowPair {
+    int64_t step;    // bytes from row (t, b) to (t + 1, b)
+    int64_t base;    // bytes of row (0, b)
+    __device__ __forceinline__ RowPair(int64_t ld, int B, int b, int es) : step(int64_t(B) * ld * es), base(b * ld * es) {}
+    template <typename T>
+    __device__ __forceinline__ T* at(T* p, int t, uint32_t d, bool second) const {
+        char* row = uniform(reinterpret_cast<char*>(const_cast<std::remove_const_t<T>*>(p)) + base + t * step);
+        return reinterpret_cast<T*>(row + (d * uint32_t(sizeof(T)) + (second ? uint32_t(step) : 0u)));
+    }
+};
+
+// Backward of one segment.  A wave has 32 channels, 2 to a lane (lane l: channels
+// 2 (l % 16) + [0, 2)), and the states in four parts over the wave's 16-lane
+// rows, so that the sums over states and those over channels (for dB and dC)
+// both lie half in-lane and half across lanes.  Two steps' sums over states are
+// folded together, which leaves lane l with channel 2 (l % 16) + l / 16 % 2 of
+// step l / 32: there it does the work per channel (step size, gate, loads and
+// stores).  Values cross between the two layouts in LDS.  Chunks go backwards;
+// the states inside one are formed again from its start.
 template <typename T, int NP, bool GATE>
-__global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a, SeqSlice s) {
-    constexpr int CK = chunk_steps(NP), NL = NP / 4, W = 4;
+__global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a, SeqSlice s) {
+    constexpr int CK = chunk_steps(NP), NL = NP / 4, P = CK / 2;
     __shared__ float bc[CK * 2 * NP];
-    __shared__ float red[W][CK][2 * NP];
-    __shared__ float sh[W][GATE ? 6 : 5][CK][64];   // e, u, gy, x, de/dv, and with a gate dy silu'(z)
+    __shared__ float red[kBwdWaves][CK][2 * NP];
+    __shared__ float sh[kBwdWaves][3][CK][32];   // e, u, gy
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int c16 = lane & 15, ng = lane >> 4;
-    const int group = blockIdx.x / a.blocks, blk = blockIdx.x % a.blocks, tile = blk * waves + wave;
-    const int own = 4 * c16 + ng;
-    const bool live = tile * 64 + own < a.Dg;
-    const int d = group * a.Dg + (live ? tile * 64 + own : 0);
+    const int group = blockIdx.x / a.bblocks, blk = blockIdx.x % a.bblocks, ch0 = (blk * waves + wave) * 32;
+    const int own = 2 * c16 + (ng & 1), half = ng >> 1;
+    const bool live = ch0 + own < a.Dg;
+    const uint32_t d = group * a.Dg + (live ? ch0 + own : 0);
     const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
-    const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg);
-    float A2[4][NL], g[4][NL], dA[4][NL];
-    int dc[4];   // the lane's channels in the state layout, and whether they exist
-    bool dl[4];
+    const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg), lim = min(len, t1);
+    float A2[2][NL], g[2][NL], dA[2][NL];
+    // the lane's channels in the state layout: d2 + r for r < n2
+    const uint32_t d2 = group * a.Dg + min(ch0 + 2 * c16, a.Dg - 1);
+    const int n2 = a.Dg - (ch0 + 2 * c16);
+    // its states in the rows [quarter][d][4] from p
+    auto load_states = [&](const float* p, float (&v)[2][NL]) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int ch = tile * 64 + 4 * c16 + r;
-        dl[r] = ch < a.Dg;
-        dc[r] = group * a.Dg + (dl[r] ? ch : 0);
+        for (int r = 0; r < 2; ++r) {
+            const uint32_t dr = min(d2 + r, uint32_t(a.D - 1));
+            if constexpr (NL >= 4) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int n = ng * NL + i;
-            const bool on = dl[r] && n < a.N;
-            A2[r][i] = on ? a.A[int64_t(dc[r]) * a.N + n] * kLog2e : 0.f;
-            dA[r][i] = 0.f;
-            g[r][i] = 0.f;
-            if (on) {
-                if (a.nseg > 1) g[r][i] = state_at<NP>(a.seg_g, a, seg, b, n / 4, dc[r])[n % 4];
-                else if (a.dhT) g[r][i] = a.dhT[(int64_t(b) * a.D + dc[r]) * a.N + n];
+                for (int q = 0; q < NL / 4; ++q) {
+                    const float4 f = reinterpret_cast<const float4*>(p)[uint32_t(ng * (NL / 4) + q) * a.D + dr];
+                    v[r][4 * q] = f.x, v[r][4 * q + 1] = f.y, v[r][4 * q + 2] = f.z, v[r][4 * q + 3] = f.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const int n = ng * NL + i;
+                    v[r][i] = p[(uint32_t(n / 4) * a.D + dr) * 4 + n % 4];
+                }
             }
+#pragma unroll
+            for (int i = 0; i < NL; ++i) v[r][i] = r < n2 ? v[r][i] : 0.f;
         }
-    }
+    };
+    // the same from a dense [D, N], 0 where it is NULL
+    auto load_dense = [&](const float* p, float (&v)[2][NL]) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < NL; ++i)
+                v[r][i] = p && r < n2 && ng * NL + i < a.N ? p[(d2 + r) * a.N + ng * NL + i] : 0.f;
+    };
+    load_dense(a.A, A2);
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < NL; ++i) A2[r][i] *= kLog2e, dA[r][i] = 0.f;
+    const int64_t bstate = int64_t(b) * a.D * a.N;
+    if (a.nseg > 1) load_states(uniform(state_at<NP>(a.seg_g, a, seg, b, 0, 0)), g);
+    else load_dense(a.dhT ? a.dhT + bstate : nullptr, g);
     const float dskip = a.Dskip ? a.Dskip[d] : 0.f, dtb = a.dtb ? a.dtb[d] : 0.f;
-    const T* xp = static_cast<const T*>(a.x) + b * a.ldx + d;
-    const T* tp = static_cast<const T*>(a.dt) + b * a.ldt + d;
-    const T* zp = GATE ? static_cast<const T*>(a.z) + b * a.ldz + d : nullptr;
-    const T* gp = static_cast<const T*>(a.dy) + b * a.ldy + d;
-    T* dxp = static_cast<T*>(a.dx) + b * a.ldx + d;
-    T* dtp = static_cast<T*>(a.ddt) + b * a.ldt + d;
-    T* dzp = GATE ? static_cast<T*>(a.dz) + b * a.ldz + d : nullptr;
-    const int64_t sx = a.B * a.ldx, st = a.B * a.ldt, sz = a.B * a.ldz, sy = a.B * a.ldy;
+    const T *X = static_cast<const T*>(a.x), *DT = static_cast<const T*>(a.dt), *Z = static_cast<const T*>(a.z),
+            *DY = static_cast<const T*>(a.dy);
+    T *DX = static_cast<T*>(a.dx), *DDT = static_cast<T*>(a.ddt), *DZ = static_cast<T*>(a.dz);
+    const RowPair rx(a.ldx, a.B, b, sizeof(T)), rt(a.ldt, a.B, b, sizeof(T)), rz(a.ldz, a.B, b, sizeof(T)),
+        ry(a.ldy, a.B, b, sizeof(T));
     float dD = 0.f, dtbs = 0.f;
     for (int tc = t0 + (t1 - 1 - t0) / CK * CK; tc >= t0; tc -= CK) {
         const int tn = min(CK, t1 - tc);
+        float ox[P], osv[P], ozf[P];   // the lane's channel in steps 2 i + half: x, de/dv, dy silu'(z)
         if (tc < len) {
-            // the work per channel of the chunk's steps
+            T vx[P], vt[P], vg[P], vz[P];   // (past the end: the last row's values, not used)
 #pragma unroll
-            for (int i = 0; i < CK; ++i) {
-                float e = 0.f, u = 0.f, gy = 0.f, x = 0.f, sv = 0.f, zf = 0.f;
-                if (tc + i < min(len, t1) && live) {
-                    x = to_f(xp[(tc + i) * sx]);
-                    const float v = to_f(tp[(tc + i) * st]) + dtb;
-                    e = step_size(v, a.softplus);
-                    sv = a.softplus ? sigmoidf_(v) : 1.f;
-                    u = e * x;
-                    gy = to_f(gp[(tc + i) * sy]);
-                    if (GATE) {
-                        const float z = to_f(zp[(tc + i) * sz]), q = sigmoidf_(z);
-                        zf = gy * q * (1.f + z * (1.f - q));
-                        gy *= z * q;
-                    }
-                }
-                sh[wave][0][i][own] = e;
-                sh[wave][1][i][own] = u;
-                sh[wave][2][i][own] = gy;
-                sh[wave][3][i][own] = x;
-                sh[wave][4][i][own] = sv;
-                if (GATE) sh[wave][GATE ? 5 : 0][i][own] = zf;
+            for (int i = 0; i < P; ++i) {
+                const int t = min(tc + 2 * i, lim - 1);
+                const bool second = half && tc + 2 * i + 1 < lim;
+                vx[i] = *rx.at(X, t, d, second);
+                vt[i] = *rt.at(DT, t, d, second);
+                vg[i] = *ry.at(DY, t, d, second);
+                if (GATE) vz[i] = *rz.at(Z, t, d, second);
             }
-            stage_bc<T, NP>(a, bc, tc, CK, min(len, t1), b, group);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const int k = 2 * i + half;
+                const bool on = tc + k < lim && live;
+                const float x = on ? to_f(vx[i]) : 0.f, v = to_f(vt[i]) + dtb;
+                const float e = on ? step_size(v, a.softplus) : 0.f;
+                float gy = on ? to_f(vg[i]) : 0.f;
+                ox[i] = x;
+                osv[i] = !on ? 0.f : a.softplus ? sigmoidf_(v) : 1.f;
+                if (GATE) {
+                    const float z = on ? to_f(vz[i]) : 0.f, q = sigmoidf_(z);
+                    ozf[i] = gy * q * (1.f + z * (1.f - q));
+                    gy *= z * q;
+                }
+                sh[wave][0][k][own] = e;
+                sh[wave][1][k][own] = e * x;
+                sh[wave][2][k][own] = gy;
+            }
+            stage_bc<T, NP>(a, bc, tc, CK, lim, b, group);
         }
         __syncthreads();
         if (tc < len) {
             // states of the chunk: h[i] before its step i
-            float h[CK + 1][4][NL];
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int i = 0; i < NL; ++i) {
-                    const int n = ng * NL + i;
-                    h[0][r][i] = 0.f;
-                    if (dl[r] && n < a.N) {
-                        if (tc > 0) h[0][r][i] = state_at<NP>(a.ck, a, tc / CK - 1, b, n / 4, dc[r])[n % 4];
-                        else if (a.h0) h[0][r][i] = a.h0[(int64_t(b) * a.D + dc[r]) * a.N + n];
-                    }
-                }
+            float h[CK + 1][2][NL];
+            if (tc > 0) load_states(uniform(state_at<NP>(a.ck, a, tc / CK - 1, b, 0, 0)), h[0]);
+            else load_dense(a.h0 ? a.h0 + bstate : nullptr, h[0]);
 #pragma unroll
             for (int k = 0; k < CK; ++k) {
-                const float4 e4 = *reinterpret_cast<const float4*>(&sh[wave][0][k][4 * c16]);
-                const float4 u4 = *reinterpret_cast<const float4*>(&sh[wave][1][k][4 * c16]);
-                const float e[4] = {e4.x, e4.y, e4.z, e4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+                const float2 e2 = *reinterpret_cast<const float2*>(&sh[wave][0][k][2 * c16]);
+                const float2 u2 = *reinterpret_cast<const float2*>(&sh[wave][1][k][2 * c16]);
+                const float e[2] = {e2.x, e2.y}, u[2] = {u2.x, u2.y};
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
                     const float bn = bc[k * 2 * NP + ng * NL + i];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) h[k + 1][r][i] = fmaf(exp2_(e[r] * A2[r][i]), h[k][r][i], u[r] * bn);
+                    for (int r = 0; r < 2; ++r) h[k + 1][r][i] = fmaf(exp2_(e[r] * A2[r][i]), h[k][r][i], u[r] * bn);
                 }
             }
+            forget_lds();
+            float odd[3];   // the odd step's sums over states, folded once
 #pragma unroll
             for (int k = CK - 1; k >= 0; --k) {
-                const float4 e4 = *reinterpret_cast<const float4*>(&sh[wave][0][k][4 * c16]);
-                const float4 u4 = *reinterpret_cast<const float4*>(&sh[wave][1][k][4 * c16]);
-                const float4 g4 = *reinterpret_cast<const float4*>(&sh[wave][2][k][4 * c16]);
-                const float e[4] = {e4.x, e4.y, e4.z, e4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
-                const float gy[4] = {g4.x, g4.y, g4.z, g4.w};
-                float bcs[2 * NL], sb[4] = {}, sa[4] = {}, yr[4] = {};
+                __builtin_amdgcn_sched_barrier(0);
+                const float2 e2 = *reinterpret_cast<const float2*>(&sh[wave][0][k][2 * c16]);
+                const float2 u2 = *reinterpret_cast<const float2*>(&sh[wave][1][k][2 * c16]);
+                const float2 g2 = *reinterpret_cast<const float2*>(&sh[wave][2][k][2 * c16]);
+                const float e[2] = {e2.x, e2.y}, u[2] = {u2.x, u2.y}, gy[2] = {g2.x, g2.y};
+                float bcs[2 * NL], sb[2] = {}, sa[2] = {}, yr[2] = {};
 #pragma unroll
                 for (int i = 0; i < 2 * NL; ++i) bcs[i] = 0.f;
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
                     const float bn = bc[k * 2 * NP + ng * NL + i], cn = bc[k * 2 * NP + NP + ng * NL + i];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
+                    for (int r = 0; r < 2; ++r) {
                         const float gn = fmaf(gy[r], cn, g[r][i]);
                         bcs[NL + i] = fmaf(gy[r], h[k + 1][r][i], bcs[NL + i]);
                         bcs[i] = fmaf(gn, u[r], bcs[i]);
@@ -481,24 +533,30 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a, SeqSlice s
                         red[wave][k][(m < NL ? 0 : NP - NL) + ng * NL + m] = bcs[j];
                     }
                 }
-                const float S = fold_rows(sb), R = fold_rows(sa) * kLn2;
-                const float oe = sh[wave][0][k][own], ogy = sh[wave][2][k][own], ox = sh[wave][3][k][own];
-                const float ddt = (ox * S + R) * sh[wave][4][k][own];
-                dD += ogy * ox;
-                dtbs += ddt;
-                float dz = 0.f;
-                if (GATE) dz = sh[wave][GATE ? 5 : 0][k][own] * fmaf(dskip, ox, fold_rows(yr));
-                if (k < tn && live) {   // 0 past the sequence's end: e, u, gy, x are
-                    dxp[(tc + k) * sx] = out_f<T>(fmaf(ogy, dskip, oe * S));
-                    dtp[(tc + k) * st] = out_f<T>(ddt);
-                    if (GATE) dzp[(tc + k) * sz] = out_f<T>(dz);
+                const float fs = fold16(sb[0], sb[1]), fa = fold16(sa[0], sa[1]), fy = GATE ? fold16(yr[0], yr[1]) : 0.f;
+                if (k & 1) {
+                    odd[0] = fs, odd[1] = fa, odd[2] = fy;
+                } else {
+                    const float S = fold32(fs, odd[0]), R = fold32(fa, odd[1]) * kLn2;
+                    const float oe = sh[wave][0][k + half][own], ogy = sh[wave][2][k + half][own];
+                    const float x = ox[k / 2], ddt = (x * S + R) * osv[k / 2];
+                    dD += ogy * x;
+                    dtbs += ddt;
+                    float dz = 0.f;
+                    if (GATE) dz = ozf[k / 2] * fmaf(dskip, x, fold32(fy, odd[2]));
+                    if (k + half < tn && live) {   // 0 past the sequence's end: e, u, gy, x are
+                        *rx.at(DX, tc + k, d, half) = out_f<T>(fmaf(ogy, dskip, oe * S));
+                        *rt.at(DDT, tc + k, d, half) = out_f<T>(ddt);
+                        if (GATE) *rz.at(DZ, tc + k, d, half) = out_f<T>(dz);
+                    }
                 }
             }
         } else if (live) {
-            for (int k = 0; k < tn; ++k) {
-                dxp[(tc + k) * sx] = out_f<T>(0.f);
-                dtp[(tc + k) * st] = out_f<T>(0.f);
-                if (GATE) dzp[(tc + k) * sz] = out_f<T>(0.f);
+            for (int k = 0; k < tn; k += 2) {
+                if (k + half >= tn) continue;
+                *rx.at(DX, tc + k, d, half) = out_f<T>(0.f);
+                *rt.at(DDT, tc + k, d, half) = out_f<T>(0.f);
+                if (GATE) *rz.at(DZ, tc + k, d, half) = out_f<T>(0.f);
             }
         }
         __syncthreads();
@@ -507,26 +565,28 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_kernel(ScanArgs a, SeqSlice s
             float v = 0.f;
             if (tc + k < len)
                 for (int w = 0; w < waves; ++w) v += red[w][k][m];
-            const int64_t row = int64_t(tc + k) * a.B + b;
+            const int64_t r = int64_t(tc + k) * a.B + b;
             if (a.bc_part) {
-                a.bc_part[((int64_t(blk) * a.T * a.B + row) * a.G + group) * 2 * NP + m] = v;
+                a.bc_part[((int64_t(blk) * a.T * a.B + r) * a.G + group) * 2 * NP + m] = v;
             } else if (n < a.N) {
-                if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = out_f<T>(v);
-                else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = out_f<T>(v);
+                if (m < NP) static_cast<T*>(a.dBm)[r * a.ldb + int64_t(group) * a.N + n] = out_f<T>(v);
+                else static_cast<T*>(a.dCm)[r * a.ldc + int64_t(group) * a.N + n] = out_f<T>(v);
             }
         }
     }
     const int64_t part = int64_t(seg) * a.B + b;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 2; ++r)
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int n = ng * NL + i;
-            if (!dl[r] || n >= a.N) continue;
-            a.dA_part[(part * a.D + dc[r]) * a.N + n] = dA[r][i];
-            if (a.dh0 && seg == 0) a.dh0[(int64_t(b) * a.D + dc[r]) * a.N + n] = g[r][i];
+            if (r >= n2 || n >= a.N) continue;
+            a.dA_part[(part * a.D + d2 + r) * a.N + n] = dA[r][i];
+            if (a.dh0 && seg == 0) a.dh0[bstate + int64_t(d2 + r) * a.N + n] = g[r][i];
         }
-    if (live) {
+    dD += __shfl_xor(dD, 32, 64);
+    dtbs += __shfl_xor(dtbs, 32, 64);
+    if (live && half == 0) {
         a.dv_part[part * 2 * a.D + d] = dD;
         a.dv_part[(part * 2 + 1) * a.D + d] = dtbs;
     }
@@ -559,7 +619,7 @@ __global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a) {
     const int64_t row = i / (2 * NP) / a.G;
     if (n >= a.N) return;
     float v = 0.f;
-    for (int k = 0; k < a.blocks; ++k) v += a.bc_part[k * all + i];
+    for (int k = 0; k < a.bblocks; ++k) v += a.bc_part[k * all + i];
     if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = out_f<T>(v);
     else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = out_f<T>(v);
 }
@@ -637,7 +697,8 @@ bool scan_desc_ok(const janus_scan_desc* d) {
 }
 bool scan_supported(const janus_scan_desc* d) {
     return dtype_ok(d->dtype) && d->N <= kMaxStates && (d->flags & ~(JANUS_SCAN_SOFTPLUS | JANUS_SCAN_KEEP)) == 0 &&
-           d->T <= (1 << 30) && d->D <= (1 << 24) && d->B <= (1 << 24);
+           d->T <= (1 << 30) && d->D <= (1 << 22) && d->B <= (1 << 24) &&
+           d->B * std::max({d->ldx, d->ldt, d->ldz, d->ldy, int64_t(d->D)}) <= (int64_t(1) << 29);
 }
 // states rounded up to what the kernels are built for
 int padded_states(int N) { return N <= 4 ? 4 : N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
@@ -655,6 +716,8 @@ ScanArgs scan_geometry(const janus_scan_desc* d) {
     a.softplus = d->flags & JANUS_SCAN_SOFTPLUS;
     a.tiles = (a.Dg + 63) / 64;
     a.blocks = (a.tiles + kScanWaves - 1) / kScanWaves;
+    a.btiles = (a.Dg + 31) / 32;
+    a.bblocks = (a.btiles + kBwdWaves - 1) / kBwdWaves;
     // With fewer waves than the chip's 1024 SIMDs the time axis is cut, into segments of 64 steps
     // and more, for two waves a SIMD: the cut costs a second pass over the inputs.
     const int64_t waves = int64_t(a.B) * a.G * a.tiles;
@@ -679,7 +742,7 @@ size_t scan_carve(ScanArgs& a, bool keep, void* ws) {
         if (a.nseg > 1) a.seg_g = c.take<float>(a.nseg * state);
         a.dA_part = c.take<float>(parts * a.D * a.N);
         a.dv_part = c.take<float>(parts * 2 * a.D);
-        if (a.blocks > 1) a.bc_part = c.take<float>(size_t(a.blocks) * a.T * a.B * a.G * 2 * NP);
+        if (a.bblocks > 1) a.bc_part = c.take<float>(size_t(a.bblocks) * a.T * a.B * a.G * 2 * NP);
     }
     return c.off;
 }
@@ -751,9 +814,9 @@ janus_status scan_bwd_run(const ScanArgs& a, const int32_t* lengths, float* dA, 
         SeqSlice s;
         const int n = fill_slice(s, b0, a.B, a.T, lengths);
         TraceScope trace("scan_bwd", el / a.B * n * 24 * a.N, el / a.B * n * (a.z ? 7 : 5) * sizeof(T), st);
-        const dim3 grid(a.blocks * a.G, n, a.nseg);
-        if (a.z) hipLaunchKernelGGL((scan_bwd_kernel<T, NP, true>), grid, scan_block(a), 0, st, a, s);
-        else hipLaunchKernelGGL((scan_bwd_kernel<T, NP, false>), grid, scan_block(a), 0, st, a, s);
+        const dim3 grid(a.bblocks * a.G, n, a.nseg), block(64 * std::min(kBwdWaves, a.btiles));
+        if (a.z) hipLaunchKernelGGL((scan_bwd_kernel<T, NP, true>), grid, block, 0, st, a, s);
+        else hipLaunchKernelGGL((scan_bwd_kernel<T, NP, false>), grid, block, 0, st, a, s);
         JANUS_LAUNCH_CHECK();
     }
     const int64_t np = int64_t(a.D) * a.N + 2 * a.D;
@@ -766,7 +829,7 @@ janus_status scan_bwd_run(const ScanArgs& a, const int32_t* lengths, float* dA, 
     }
     if (a.bc_part && a.T > 0) {
         const int64_t all = int64_t(a.T) * a.B * a.G * 2 * NP;
-        TraceScope trace("scan_bc", double(all) * a.blocks, 4.0 * all * a.blocks, st);
+        TraceScope trace("scan_bc", double(all) * a.bblocks, 4.0 * all * a.bblocks, st);
         hipLaunchKernelGGL((scan_bc_kernel<T, NP>), dim3((all + 255) / 256), dim3(256), 0, st, a);
         JANUS_LAUNCH_CHECK();
     }
