@@ -28,9 +28,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxStates = 64;
 constexpr int kStage = 32;    // steps whose B and C rows lie in LDS at once
 
-// Steps between two kept states: the backward holds the states of one such
-// chunk in registers (128 floats a lane for 16 states and more).
-constexpr int chunk_steps(int NP) { return NP <= 8 ? 16 : 128 / NP; }
+// Steps between two kept states.  Fewer cost more bytes (a kept state is NP
+// floats a channel), more cost the backward registers for the states between.
+constexpr int chunk_steps(int NP) { return NP <= 8 ? 16 : NP <= 32 ? 8 : 4; }
 #ifndef MW
 #define MW 2
 #endif
@@ -84,7 +84,8 @@ __device__ __forceinline__ P* uniform(P* p) {
     const uint64_t v = reinterpret_cast<uint64_t>(p);
     const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v));
     const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(v >> 32));
-    return reinterpret_cast<P*>(uint64_t(hi) << 32 | lo);
+    // (through a global pointer: an integer alone would make it a flat access)
+    return (P*)(__attribute__((address_space(1))) P*)(uint64_t(hi) << 32 | lo);
 }
 
 // [seg or chunk][b][quarter][d][4]
@@ -356,6 +357,14 @@ struct RowFold {
     }
 };
 
+// A value that the compiler takes for new where this stands, so that what is
+// computed from it (addresses above all) is computed there and not held in
+// registers from before the loop on.
+__device__ __forceinline__ uint32_t fresh(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // What was read from LDS before is read again after: keeps the compiler from
 // holding a chunk's decays in registers beside its states.
 __device__ __forceinline__ void forget_lds() { asm volatile("" ::: "memory"); }
@@ -383,7 +392,7 @@ struct RowPair {
 // the states inside one are formed again from its start.
 template <typename T, int NP, bool GATE>
 __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a, SeqSlice s) {
-    constexpr int CK = chunk_steps(NP), NL = NP / 4, P = CK / 2;
+    constexpr int CK = chunk_steps(NP), NL = NP / 4, P = CK / 2, HK = CK / 2;
     __shared__ float bc[CK * 2 * NP];
     __shared__ float red[kBwdWaves][CK][2 * NP];
     __shared__ float sh[kBwdWaves][3][CK][32];   // e, u, gy
@@ -401,9 +410,10 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
     const int n2 = a.Dg - (ch0 + 2 * c16);
     // its states in the rows [quarter][d][4] from p
     auto load_states = [&](const float* p, float (&v)[2][NL]) {
+        const uint32_t df = fresh(d2);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const uint32_t dr = min(d2 + r, uint32_t(a.D - 1));
+            const uint32_t dr = min(df + r, uint32_t(a.D - 1));
             if constexpr (NL >= 4) {
 #pragma unroll
                 for (int q = 0; q < NL / 4; ++q) {
@@ -423,11 +433,12 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
     };
     // the same from a dense [D, N], 0 where it is NULL
     auto load_dense = [&](const float* p, float (&v)[2][NL]) {
+        const uint32_t df = fresh(d2);
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int i = 0; i < NL; ++i)
-                v[r][i] = p && r < n2 && ng * NL + i < a.N ? p[(d2 + r) * a.N + ng * NL + i] : 0.f;
+                v[r][i] = p && r < n2 && ng * NL + i < a.N ? p[(df + r) * a.N + ng * NL + i] : 0.f;
     };
     load_dense(a.A, A2);
 #pragma unroll
@@ -480,12 +491,12 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
         }
         __syncthreads();
         if (tc < len) {
-            // states of the chunk: h[i] before its step i
-            float h[CK + 1][2][NL];
-            if (tc > 0) load_states(uniform(state_at<NP>(a.ck, a, tc / CK - 1, b, 0, 0)), h[0]);
-            else load_dense(a.h0 ? a.h0 + bstate : nullptr, h[0]);
-#pragma unroll
-            for (int k = 0; k < CK; ++k) {
+            // Half a chunk at a time, the later one first: h[i] is the state before the half's step i.  (The
+            // earlier half's steps run twice; holding a whole chunk's states would leave two waves a SIMD.)
+            float start[2][NL], h[HK + 1][2][NL];
+            if (tc > 0) load_states(uniform(state_at<NP>(a.ck, a, tc / CK - 1, b, 0, 0)), start);
+            else load_dense(a.h0 ? a.h0 + bstate : nullptr, start);
+            auto advance = [&](int k, const float (&from)[2][NL], float (&to)[2][NL]) {
                 const float2 e2 = *reinterpret_cast<const float2*>(&sh[wave][0][k][2 * c16]);
                 const float2 u2 = *reinterpret_cast<const float2*>(&sh[wave][1][k][2 * c16]);
                 const float e[2] = {e2.x, e2.y}, u[2] = {u2.x, u2.y};
@@ -493,13 +504,30 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
                 for (int i = 0; i < NL; ++i) {
                     const float bn = bc[k * 2 * NP + ng * NL + i];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) h[k + 1][r][i] = fmaf(exp2_(e[r] * A2[r][i]), h[k][r][i], u[r] * bn);
+                    for (int r = 0; r < 2; ++r) to[r][i] = fmaf(exp2_(e[r] * A2[r][i]), from[r][i], u[r] * bn);
                 }
-            }
-            forget_lds();
+            };
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int i = 0; i < NL; ++i) h[0][r][i] = start[r][i];
+#pragma unroll
+            for (int k = 0; k < HK; ++k) advance(k, h[0], h[0]);
             float odd[3];   // the odd step's sums over states, folded once
 #pragma unroll
-            for (int k = CK - 1; k >= 0; --k) {
+            for (int k0 = HK; k0 >= 0; k0 -= HK) {
+            if (k0 == 0) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < NL; ++i) h[0][r][i] = start[r][i];
+            }
+            forget_lds();
+#pragma unroll
+            for (int k = 0; k < HK; ++k) advance(k0 + k, h[k], h[k + 1]);
+            forget_lds();
+#pragma unroll
+            for (int k = k0 + HK - 1; k >= k0; --k) {
                 __builtin_amdgcn_sched_barrier(0);
                 const float2 e2 = *reinterpret_cast<const float2*>(&sh[wave][0][k][2 * c16]);
                 const float2 u2 = *reinterpret_cast<const float2*>(&sh[wave][1][k][2 * c16]);
@@ -514,16 +542,21 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const float gn = fmaf(gy[r], cn, g[r][i]);
-                        bcs[NL + i] = fmaf(gy[r], h[k + 1][r][i], bcs[NL + i]);
+                        bcs[NL + i] = fmaf(gy[r], h[k - k0 + 1][r][i], bcs[NL + i]);
                         bcs[i] = fmaf(gn, u[r], bcs[i]);
                         sb[r] = fmaf(gn, bn, sb[r]);
-                        if (GATE) yr[r] = fmaf(h[k + 1][r][i], cn, yr[r]);
-                        const float w = gn * exp2_(e[r] * A2[r][i]), q = w * h[k][r][i];
+                        if (GATE) yr[r] = fmaf(h[k - k0 + 1][r][i], cn, yr[r]);
+                        const float w = gn * exp2_(e[r] * A2[r][i]), q = w * h[k - k0][r][i];
                         sa[r] = fmaf(q, A2[r][i], sa[r]);
                         dA[r][i] = fmaf(q, e[r], dA[r][i]);
                         g[r][i] = w;
                     }
                 }
+                // (left alone, the compiler puts dA off to the chunk's end and keeps every step's terms)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < NL; ++i) asm volatile("" : "+v"(dA[r][i]));
                 RowFold<2 * NL>::run(bcs, lane);
                 if (RowFold<2 * NL>::writes(lane)) {
                     const int f = RowFold<2 * NL>::first(c16);
@@ -551,6 +584,7 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
                     }
                 }
             }
+            }
         } else if (live) {
             for (int k = 0; k < tn; k += 2) {
                 if (k + half >= tn) continue;
@@ -560,7 +594,7 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
             }
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < tn * 2 * NP; i += blockDim.x) {
+        for (int i = fresh(threadIdx.x); i < tn * 2 * NP; i += blockDim.x) {
             const int k = i / (2 * NP), m = i % (2 * NP), n = m % NP;
             float v = 0.f;
             if (tc + k < len)
@@ -575,14 +609,15 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
         }
     }
     const int64_t part = int64_t(seg) * a.B + b;
+    const uint32_t df = fresh(d2);
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int n = ng * NL + i;
             if (r >= n2 || n >= a.N) continue;
-            a.dA_part[(part * a.D + d2 + r) * a.N + n] = dA[r][i];
-            if (a.dh0 && seg == 0) a.dh0[bstate + int64_t(d2 + r) * a.N + n] = g[r][i];
+            a.dA_part[(part * a.D + df + r) * a.N + n] = dA[r][i];
+            if (a.dh0 && seg == 0) a.dh0[bstate + int64_t(df + r) * a.N + n] = g[r][i];
         }
     dD += __shfl_xor(dD, 32, 64);
     dtbs += __shfl_xor(dtbs, 32, 64);
