@@ -31,6 +31,9 @@ constexpr int kStage = 32;    // steps whose B and C rows lie in LDS at once
 // Steps between two kept states.  Fewer cost more bytes (a kept state is NP
 // floats a channel), more cost the backward registers for the states between.
 constexpr int chunk_steps(int NP) { return NP <= 8 ? 16 : NP <= 32 ? 8 : 4; }
+#ifndef HD
+#define HD 2
+#endif
 #ifndef MW
 #define MW 2
 #endif
@@ -110,8 +113,20 @@ __device__ __forceinline__ void stage_bc(const ScanArgs& a, float* lds, int t, i
     }
 }
 
-// One lane per channel, its NP states in registers; B and C come from LDS,
-// the same address in all lanes.  LOCAL: only the state at the segment's end
+// Rows (t, b) of an operand: a uniform address, to which a lane adds its channel.
+struct Rows {
+    int64_t step, base;    // bytes from row (t, b) to (t + 1, b), of row (0, b)
+    __device__ __forceinline__ Rows(int64_t ld, int B, int b, int es) : step(int64_t(B) * ld * es), base(b * ld * es) {}
+    template <typename T>
+    __device__ __forceinline__ T* at(T* p, int t) const {
+        return reinterpret_cast<T*>(
+            uniform(reinterpret_cast<char*>(const_cast<std::remove_const_t<T>*>(p)) + base + t * step));
+    }
+};
+
+// One lane per channel, its NP states in registers; B and C come from LDS, the
+// same address in all lanes.  Eight steps at a time: their rows are loaded while
+// the eight before are worked on.  LOCAL: only the state at the segment's end
 // from a zero start, and the sum of e.
 template <typename T, int NP, bool LOCAL>
 __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
@@ -121,13 +136,13 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
     const int group = blockIdx.x / a.blocks, tile = (blockIdx.x % a.blocks) * waves + wave;
     const int ch = tile * 64 + lane;
     const bool live = ch < a.Dg;
-    const int d = group * a.Dg + (live ? ch : 0);
+    const uint32_t d = group * a.Dg + (live ? ch : 0);
     const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
     const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg), te = min(t1, len);
     float A2[NP], h[NP];
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
-        A2[n] = n < a.N ? a.A[int64_t(d) * a.N + n] * kLog2e : 0.f;
+        A2[n] = n < a.N ? a.A[d * a.N + n] * kLog2e : 0.f;
         h[n] = 0.f;
     }
     if (!LOCAL && seg > 0) {
@@ -142,53 +157,62 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
             if (n < a.N) h[n] = a.h0[(int64_t(b) * a.D + d) * a.N + n];
     }
     const float dskip = a.Dskip ? a.Dskip[d] : 0.f, dtb = a.dtb ? a.dtb[d] : 0.f;
-    const T* xp = static_cast<const T*>(a.x) + b * a.ldx + d;
-    const T* tp = static_cast<const T*>(a.dt) + b * a.ldt + d;
-    const T* zp = a.z ? static_cast<const T*>(a.z) + b * a.ldz + d : nullptr;
-    T* yp = LOCAL ? nullptr : static_cast<T*>(a.y) + b * a.ldy + d;
-    const int64_t sx = a.B * a.ldx, st = a.B * a.ldt, sz = a.B * a.ldz, sy = a.B * a.ldy;
+    const T *X = static_cast<const T*>(a.x), *DT = static_cast<const T*>(a.dt), *Z = static_cast<const T*>(a.z);
+    T* Y = static_cast<T*>(a.y);
+    const Rows rx(a.ldx, a.B, b, sizeof(T)), rt(a.ldt, a.B, b, sizeof(T)), rz(a.ldz, a.B, b, sizeof(T)),
+        ry(a.ldy, a.B, b, sizeof(T));
+    const bool gate = !LOCAL && Z;
     float esum = 0.f;
+    T nx[U], nt[U], nz[U];   // rows on their way (past the end: the last one again, not used)
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int r = min(t + i, te - 1);
+            nx[i] = rx.at(X, r)[d];
+            nt[i] = rt.at(DT, r)[d];
+            if (gate) nz[i] = rz.at(Z, r)[d];
+        }
+    };
+    if (t0 < te) fetch(t0);
     for (int ts = t0; ts < te; ts += kStage) {
         __syncthreads();
         stage_bc<T, NP>(a, bc, ts, min(kStage, te - ts), te, b, group);
         __syncthreads();
         for (int tu = ts; tu < min(te, ts + kStage); tu += U) {
-            T rx[U], rt[U], rz[U];
+            float x[U], e[U], z[U];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                if (tu + i < te && live) {
-                    rx[i] = xp[(tu + i) * sx];
-                    rt[i] = tp[(tu + i) * st];
-                    if (!LOCAL && zp) rz[i] = zp[(tu + i) * sz];
-                }
+                const bool on = tu + i < te;
+                x[i] = on ? to_f(nx[i]) : 0.f;
+                e[i] = on ? step_size(to_f(nt[i]) + dtb, a.softplus) : 0.f;
+                if (gate) z[i] = to_f(nz[i]);
             }
+            if (tu + U < te) fetch(tu + U);
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 const int t = tu + i;
-                if (t >= te) break;
-                if (!LOCAL && a.ck && t % CK == 0 && t > 0 && live) {
+                if (!LOCAL && a.ck && i % CK == 0 && t > 0 && t < te && t % CK == 0 && live) {
+                    float4* ck = reinterpret_cast<float4*>(uniform(state_at<NP>(a.ck, a, t / CK - 1, b, 0, 0)));
 #pragma unroll
                     for (int q = 0; q < NP / 4; ++q)
-                        *reinterpret_cast<float4*>(state_at<NP>(a.ck, a, t / CK - 1, b, q, d)) =
-                            make_float4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+                        ck[uint32_t(q) * a.D + d] = make_float4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
                 }
-                const float x = to_f(rx[i]), e = step_size(to_f(rt[i]) + dtb, a.softplus), u = e * x;
+                const float u = e[i] * x[i];
                 const float* row = bc + (t - ts) * 2 * NP;
                 float y = 0.f;
+                if (t < te) {
 #pragma unroll
-                for (int n = 0; n < NP; ++n) {
-                    h[n] = fmaf(exp2_(e * A2[n]), h[n], u * row[n]);
-                    if (!LOCAL) y = fmaf(h[n], row[NP + n], y);
+                    for (int n = 0; n < NP; ++n) {
+                        h[n] = fmaf(exp2_(e[i] * A2[n]), h[n], u * row[n]);
+                        if (!LOCAL) y = fmaf(h[n], row[NP + n], y);
+                    }
                 }
                 if (LOCAL) {
-                    esum += e;
-                } else if (live) {
-                    y = fmaf(dskip, x, y);
-                    if (zp) {
-                        const float z = to_f(rz[i]);
-                        y *= z * sigmoidf_(z);
-                    }
-                    yp[t * sy] = out_f<T>(y);
+                    esum += e[i];
+                } else if (t < te) {
+                    y = fmaf(dskip, x[i], y);
+                    if (gate) y *= z[i] * sigmoidf_(z[i]);
+                    if (live) ry.at(Y, t)[d] = out_f<T>(y);
                 }
             }
         }
@@ -202,7 +226,7 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
         a.seg_e[(int64_t(seg) * a.B + b) * a.D + d] = esum;
         return;
     }
-    for (int t = max(t0, len); t < t1; ++t) yp[t * sy] = out_f<T>(0.f);
+    for (int t = max(t0, len); t < t1; ++t) ry.at(Y, t)[d] = out_f<T>(0.f);
     if (a.hT && seg == a.nseg - 1) {
 #pragma unroll
         for (int n = 0; n < NP; ++n)
@@ -392,7 +416,7 @@ struct RowPair {
 // the states inside one are formed again from its start.
 template <typename T, int NP, bool GATE>
 __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a, SeqSlice s) {
-    constexpr int CK = chunk_steps(NP), NL = NP / 4, P = CK / 2, HK = CK / 2;
+    constexpr int CK = chunk_steps(NP), NL = NP / 4, P = CK / 2, HK = CK / HD;
     __shared__ float bc[CK * 2 * NP];
     __shared__ float red[kBwdWaves][CK][2 * NP];
     __shared__ float sh[kBwdWaves][3][CK][32];   // e, u, gy
@@ -512,11 +536,11 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
 #pragma unroll
                 for (int i = 0; i < NL; ++i) h[0][r][i] = start[r][i];
 #pragma unroll
-            for (int k = 0; k < HK; ++k) advance(k, h[0], h[0]);
+            for (int k = 0; k < CK - HK; ++k) advance(k, h[0], h[0]);
             float odd[3];   // the odd step's sums over states, folded once
 #pragma unroll
-            for (int k0 = HK; k0 >= 0; k0 -= HK) {
-            if (k0 == 0) {
+            for (int k0 = CK - HK; k0 >= 0; k0 -= HK) {
+            if (HK < CK && k0 == 0) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
