@@ -81,7 +81,7 @@ template <typename T, int K, int VEC>
 __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a, SeqSlice s) {
     const int d = (blockIdx.x * blockDim.x + threadIdx.x) * VEC;
     if (d >= a.D) return;
-    const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y;
+    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y];
     const int t0 = blockIdx.z * a.seg, t1 = min(a.T, t0 + a.seg), te = min(t1, len);
     float w[K][VEC], bias[VEC], win[K][VEC];   // win[k]: input of time t - K + 1 + k
     load_taps<T, K, VEC>(a, d, w, bias);
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(512) void conv_bwd_kernel(ConvArgs a, SeqSlice s, i
     const int64_t sx = a.B * a.ldx, sy = a.B * a.ldy;
     for (int item = blockIdx.y * groups + group; on && item < items; item += gridDim.y * groups) {
         const int bs = item / a.nseg, seg = item - bs * a.nseg;
-        const int len = s.len[bs], b = s.b0 + bs;
+        const int len = s.len[bs], b = s.b0 + s.at[bs];
         const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg);
         const T* xp = static_cast<const T*>(a.x) + b * a.ldx + d;
         const T* gp = static_cast<const T*>(a.dy) + b * a.ldy + d;

@@ -30,17 +30,8 @@ constexpr int kStage = 32;    // steps whose B and C rows lie in LDS at once
 
 // Steps between two kept states.  Fewer cost more bytes (a kept state is NP
 // floats a channel), more cost the backward registers for the states between.
-constexpr int chunk_steps(int NP) { return NP <= 8 ? 16 : NP <= 32 ? 8 : 4; }
-#ifndef HD
-#define HD 2
-#endif
-#ifndef MW
-#define MW 2
-#endif
-#ifndef BW
-#define BW 4
-#endif
-constexpr int kBwdWaves = BW;
+constexpr int chunk_steps(int NP) { return NP <= 32 ? 8 : 4; }
+constexpr int kBwdWaves = 4;
 
 struct ScanArgs {
     int32_t D, N, G, Dg, B, T;
@@ -91,6 +82,14 @@ __device__ __forceinline__ P* uniform(P* p) {
     return (P*)(__attribute__((address_space(1))) P*)(uint64_t(hi) << 32 | lo);
 }
 
+// A value that the compiler takes for new where this stands, so that what is
+// computed from it (addresses above all) is computed there and not held in
+// registers from before the loop on.
+__device__ __forceinline__ uint32_t fresh(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // [seg or chunk][b][quarter][d][4]
 template <int NP>
 __device__ __forceinline__ float* state_at(float* p, const ScanArgs& a, int64_t i, int b, int q, int d) {
@@ -129,15 +128,15 @@ struct Rows {
 // the eight before are worked on.  LOCAL: only the state at the segment's end
 // from a zero start, and the sum of e.
 template <typename T, int NP, bool LOCAL>
-__global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
-    constexpr int CK = chunk_steps(NP), U = 8;
+__global__ __launch_bounds__(256, NP <= 16 ? 4 : 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
+    constexpr int CK = chunk_steps(NP), U = NP >= 64 ? 4 : 8;
     __shared__ float bc[kStage * 2 * NP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int group = blockIdx.x / a.blocks, tile = (blockIdx.x % a.blocks) * waves + wave;
     const int ch = tile * 64 + lane;
     const bool live = ch < a.Dg;
     const uint32_t d = group * a.Dg + (live ? ch : 0);
-    const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
+    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y], seg = blockIdx.z;
     const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg), te = min(t1, len);
     float A2[NP], h[NP];
 #pragma unroll
@@ -176,9 +175,10 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
     if (t0 < te) fetch(t0);
     for (int ts = t0; ts < te; ts += kStage) {
         __syncthreads();
-        stage_bc<T, NP>(a, bc, ts, min(kStage, te - ts), te, b, group);
+        stage_bc<T, NP>(a, bc, ts, kStage, te, b, group);
         __syncthreads();
         for (int tu = ts; tu < min(te, ts + kStage); tu += U) {
+            // past the end e, u and the rows of B and C are 0: the state stays
             float x[U], e[U], z[U];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
@@ -188,49 +188,55 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
                 if (gate) z[i] = to_f(nz[i]);
             }
             if (tu + U < te) fetch(tu + U);
+            float y[U];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int t = tu + i;
-                if (!LOCAL && a.ck && i % CK == 0 && t > 0 && t < te && t % CK == 0 && live) {
-                    float4* ck = reinterpret_cast<float4*>(uniform(state_at<NP>(a.ck, a, t / CK - 1, b, 0, 0)));
+                if (!LOCAL && i % CK == 0 && a.ck && tu + i > 0 && (tu + i) % CK == 0 && tu + i < te && live) {
+                    float4* ck = reinterpret_cast<float4*>(uniform(state_at<NP>(a.ck, a, (tu + i) / CK - 1, b, 0, 0)));
+                    const uint32_t df = fresh(d);
 #pragma unroll
                     for (int q = 0; q < NP / 4; ++q)
-                        ck[uint32_t(q) * a.D + d] = make_float4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+                        ck[uint32_t(q) * a.D + df] = make_float4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
                 }
+                if (NP >= 64) __builtin_amdgcn_sched_barrier(0);   // (steps side by side would not fit the registers)
                 const float u = e[i] * x[i];
-                const float* row = bc + (t - ts) * 2 * NP;
-                float y = 0.f;
-                if (t < te) {
+                const float* row = bc + (tu + i - ts) * 2 * NP;
+                y[i] = dskip * x[i];
 #pragma unroll
-                    for (int n = 0; n < NP; ++n) {
-                        h[n] = fmaf(exp2_(e[i] * A2[n]), h[n], u * row[n]);
-                        if (!LOCAL) y = fmaf(h[n], row[NP + n], y);
-                    }
+                for (int n = 0; n < NP; ++n) {
+                    h[n] = fmaf(exp2_(e[i] * A2[n]), h[n], u * row[n]);
+                    if (!LOCAL) y[i] = fmaf(h[n], row[NP + n], y[i]);
                 }
-                if (LOCAL) {
-                    esum += e[i];
-                } else if (t < te) {
-                    y = fmaf(dskip, x[i], y);
-                    if (gate) y *= z[i] * sigmoidf_(z[i]);
-                    if (live) ry.at(Y, t)[d] = out_f<T>(y);
+                if (LOCAL) esum += e[i];
+            }
+            if (!LOCAL) {
+                if (gate) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) y[i] *= z[i] * sigmoidf_(z[i]);
+                }
+                if (live) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+                        if (tu + i < te) ry.at(Y, tu + i)[d] = out_f<T>(y[i]);
                 }
             }
         }
     }
     if (!live) return;
+    const uint32_t df = fresh(d);
     if (LOCAL) {
 #pragma unroll
         for (int q = 0; q < NP / 4; ++q)
-            *reinterpret_cast<float4*>(state_at<NP>(a.seg_h, a, seg, b, q, d)) =
+            *reinterpret_cast<float4*>(state_at<NP>(a.seg_h, a, seg, b, q, df)) =
                 make_float4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
-        a.seg_e[(int64_t(seg) * a.B + b) * a.D + d] = esum;
+        a.seg_e[(int64_t(seg) * a.B + b) * a.D + df] = esum;
         return;
     }
     for (int t = max(t0, len); t < t1; ++t) ry.at(Y, t)[d] = out_f<T>(0.f);
     if (a.hT && seg == a.nseg - 1) {
 #pragma unroll
         for (int n = 0; n < NP; ++n)
-            if (n < a.N) a.hT[(int64_t(b) * a.D + d) * a.N + n] = h[n];
+            if (n < a.N) a.hT[(int64_t(b) * a.D + df) * a.N + n] = h[n];
     }
 }
 
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(256) void scan_rev_kernel(ScanArgs a, SeqSlice s) {
     const int ch = tile * 64 + lane;
     const bool live = ch < a.Dg;
     const int d = group * a.Dg + (live ? ch : 0);
-    const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
+    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y], seg = blockIdx.z;
     const int t0 = seg * a.seg, te = min(min(a.T, t0 + a.seg), len);
     float A2[NP], g[NP];
 #pragma unroll
@@ -313,16 +319,31 @@ __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
         A2[j] = n < a.N ? a.A[int64_t(d) * a.N + n] * kLog2e : 0.f;
         h[j] = n < a.N && first ? first[(int64_t(b) * a.D + d) * a.N + n] : 0.f;
     }
-    for (int k = 0; k < a.nseg; ++k) {
-        const int seg = REVERSE ? a.nseg - 1 - k : k;
-        float4* p = reinterpret_cast<float4*>(state_at<NP>(REVERSE ? a.seg_g : a.seg_h, a, seg, b, q, d));
-        const float e = a.seg_e[(int64_t(seg) * a.B + b) * a.D + d];
-        const float4 v = *p;
-        *p = make_float4(h[0], h[1], h[2], h[3]);
-        h[0] = fmaf(exp2_(e * A2[0]), h[0], v.x);
-        h[1] = fmaf(exp2_(e * A2[1]), h[1], v.y);
-        h[2] = fmaf(exp2_(e * A2[2]), h[2], v.z);
-        h[3] = fmaf(exp2_(e * A2[3]), h[3], v.w);
+    constexpr int U = 8;   // segments whose loads go out together
+    for (int k0 = 0; k0 < a.nseg; k0 += U) {
+        float4 v[U];
+        float e[U];
+        auto at = [&](int k) {
+            return reinterpret_cast<float4*>(
+                state_at<NP>(REVERSE ? a.seg_g : a.seg_h, a, REVERSE ? a.nseg - 1 - k : k, b, q, d));
+        };
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (k0 + k < a.nseg - 1) {   // (nothing flows out of the last one)
+                v[k] = *at(k0 + k);
+                e[k] = a.seg_e[(int64_t(REVERSE ? a.nseg - 1 - k0 - k : k0 + k) * a.B + b) * a.D + d];
+            }
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (k0 + k < a.nseg) {
+                *at(k0 + k) = make_float4(h[0], h[1], h[2], h[3]);
+                if (k0 + k < a.nseg - 1) {
+                    h[0] = fmaf(exp2_(e[k] * A2[0]), h[0], v[k].x);
+                    h[1] = fmaf(exp2_(e[k] * A2[1]), h[1], v[k].y);
+                    h[2] = fmaf(exp2_(e[k] * A2[2]), h[2], v[k].z);
+                    h[3] = fmaf(exp2_(e[k] * A2[3]), h[3], v[k].w);
+                }
+            }
     }
 }
 
@@ -381,28 +402,22 @@ struct RowFold {
     }
 };
 
-// A value that the compiler takes for new where this stands, so that what is
-// computed from it (addresses above all) is computed there and not held in
-// registers from before the loop on.
-__device__ __forceinline__ uint32_t fresh(uint32_t v) {
-    asm volatile("" : "+v"(v));
-    return v;
-}
-
 // What was read from LDS before is read again after: keeps the compiler from
 // holding a chunk's decays in registers beside its states.
 __device__ __forceinline__ void forget_lds() { asm volatile("" ::: "memory"); }
 
-// A row (t, b) of an operand and the one after it, t + 1: a uniform address, and
-// the 32-bit byte offset of the lane's channel in one of the two.
+// Rows (t, b) and (t + 1, b) of an operand: a uniform address, and the 32-bit
+// byte offset of the lane's channel in the one or the other.
 struct RowPair {
-    int64_t step;    // bytes from row (t, b) to (t + 1, b)
-    int64_t base;    // bytes of row (0, b)
-    __device__ __forceinline__ RowPair(int64_t ld, int B, int b, int es) : step(int64_t(B) * ld * es), base(b * ld * es) {}
+    int64_t step, base;    // bytes from row (t, b) to (t + 1, b), of row (0, b)
+    uint32_t first, mine;  // the lane's channel in row t, in its half's row
+    __device__ __forceinline__ RowPair(int64_t ld, int B, int b, int es, uint32_t d, int half)
+        : step(int64_t(B) * ld * es), base(b * ld * es), first(d * es), mine(d * es + (half ? uint32_t(step) : 0u)) {}
+    // both: there is a row t + 1
     template <typename T>
-    __device__ __forceinline__ T* at(T* p, int t, uint32_t d, bool second) const {
+    __device__ __forceinline__ T* at(T* p, int t, bool both = true) const {
         char* row = uniform(reinterpret_cast<char*>(const_cast<std::remove_const_t<T>*>(p)) + base + t * step);
-        return reinterpret_cast<T*>(row + (d * uint32_t(sizeof(T)) + (second ? uint32_t(step) : 0u)));
+        return reinterpret_cast<T*>(row + fresh(both ? mine : first));
     }
 };
 
@@ -415,18 +430,18 @@ struct RowPair {
 // stores).  Values cross between the two layouts in LDS.  Chunks go backwards;
 // the states inside one are formed again from its start.
 template <typename T, int NP, bool GATE>
-__global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a, SeqSlice s) {
-    constexpr int CK = chunk_steps(NP), NL = NP / 4, P = CK / 2, HK = CK / HD;
+__global__ __launch_bounds__(64 * kBwdWaves, NP <= 16 ? 4 : NP == 32 ? 2 : 1) void scan_bwd_kernel(ScanArgs a, SeqSlice s) {
+    constexpr int CK = chunk_steps(NP), NL = NP / 4, P = CK / 2, HK = CK / 2;
     __shared__ float bc[CK * 2 * NP];
     __shared__ float red[kBwdWaves][CK][2 * NP];
-    __shared__ float sh[kBwdWaves][3][CK][32];   // e, u, gy
+    __shared__ float sh[kBwdWaves][GATE ? 6 : 5][CK][32];   // e, u, gy, x, de/dv, and with a gate dy silu'(z)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int c16 = lane & 15, ng = lane >> 4;
     const int group = blockIdx.x / a.bblocks, blk = blockIdx.x % a.bblocks, ch0 = (blk * waves + wave) * 32;
     const int own = 2 * c16 + (ng & 1), half = ng >> 1;
     const bool live = ch0 + own < a.Dg;
     const uint32_t d = group * a.Dg + (live ? ch0 + own : 0);
-    const int len = s.len[blockIdx.y], b = s.b0 + blockIdx.y, seg = blockIdx.z;
+    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y], seg = blockIdx.z;
     const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg), lim = min(len, t1);
     float A2[2][NL], g[2][NL], dA[2][NL];
     // the lane's channels in the state layout: d2 + r for r < n2
@@ -476,22 +491,21 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
     const T *X = static_cast<const T*>(a.x), *DT = static_cast<const T*>(a.dt), *Z = static_cast<const T*>(a.z),
             *DY = static_cast<const T*>(a.dy);
     T *DX = static_cast<T*>(a.dx), *DDT = static_cast<T*>(a.ddt), *DZ = static_cast<T*>(a.dz);
-    const RowPair rx(a.ldx, a.B, b, sizeof(T)), rt(a.ldt, a.B, b, sizeof(T)), rz(a.ldz, a.B, b, sizeof(T)),
-        ry(a.ldy, a.B, b, sizeof(T));
+    const RowPair rx(a.ldx, a.B, b, sizeof(T), d, half), rt(a.ldt, a.B, b, sizeof(T), d, half),
+        rz(a.ldz, a.B, b, sizeof(T), d, half), ry(a.ldy, a.B, b, sizeof(T), d, half);
     float dD = 0.f, dtbs = 0.f;
     for (int tc = t0 + (t1 - 1 - t0) / CK * CK; tc >= t0; tc -= CK) {
         const int tn = min(CK, t1 - tc);
-        float ox[P], osv[P], ozf[P];   // the lane's channel in steps 2 i + half: x, de/dv, dy silu'(z)
         if (tc < len) {
             T vx[P], vt[P], vg[P], vz[P];   // (past the end: the last row's values, not used)
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 const int t = min(tc + 2 * i, lim - 1);
-                const bool second = half && tc + 2 * i + 1 < lim;
-                vx[i] = *rx.at(X, t, d, second);
-                vt[i] = *rt.at(DT, t, d, second);
-                vg[i] = *ry.at(DY, t, d, second);
-                if (GATE) vz[i] = *rz.at(Z, t, d, second);
+                const bool both = tc + 2 * i + 1 < lim;
+                vx[i] = *rx.at(X, t, both);
+                vt[i] = *rt.at(DT, t, both);
+                vg[i] = *ry.at(DY, t, both);
+                if (GATE) vz[i] = *rz.at(Z, t, both);
             }
 #pragma unroll
             for (int i = 0; i < P; ++i) {
@@ -500,11 +514,11 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
                 const float x = on ? to_f(vx[i]) : 0.f, v = to_f(vt[i]) + dtb;
                 const float e = on ? step_size(v, a.softplus) : 0.f;
                 float gy = on ? to_f(vg[i]) : 0.f;
-                ox[i] = x;
-                osv[i] = !on ? 0.f : a.softplus ? sigmoidf_(v) : 1.f;
+                sh[wave][3][k][own] = x;
+                sh[wave][4][k][own] = !on ? 0.f : a.softplus ? sigmoidf_(v) : 1.f;
                 if (GATE) {
                     const float z = on ? to_f(vz[i]) : 0.f, q = sigmoidf_(z);
-                    ozf[i] = gy * q * (1.f + z * (1.f - q));
+                    sh[wave][GATE ? 5 : 0][k][own] = gy * q * (1.f + z * (1.f - q));
                     gy *= z * q;
                 }
                 sh[wave][0][k][own] = e;
@@ -517,10 +531,14 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
         if (tc < len) {
             // Half a chunk at a time, the later one first: h[i] is the state before the half's step i.  (The
             // earlier half's steps run twice; holding a whole chunk's states would leave two waves a SIMD.)
-            float start[2][NL], h[HK + 1][2][NL];
-            if (tc > 0) load_states(uniform(state_at<NP>(a.ck, a, tc / CK - 1, b, 0, 0)), start);
-            else load_dense(a.h0 ? a.h0 + bstate : nullptr, start);
+            float h[HK + 1][2][NL];
+            auto load_start = [&] {
+                if (tc > 0) load_states(uniform(state_at<NP>(a.ck, a, tc / CK - 1, b, 0, 0)), h[0]);
+                else load_dense(a.h0 ? a.h0 + bstate : nullptr, h[0]);
+            };
+            load_start();
             auto advance = [&](int k, const float (&from)[2][NL], float (&to)[2][NL]) {
+                __builtin_amdgcn_sched_barrier(0);
                 const float2 e2 = *reinterpret_cast<const float2*>(&sh[wave][0][k][2 * c16]);
                 const float2 u2 = *reinterpret_cast<const float2*>(&sh[wave][1][k][2 * c16]);
                 const float e[2] = {e2.x, e2.y}, u[2] = {u2.x, u2.y};
@@ -532,20 +550,11 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
                 }
             };
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int i = 0; i < NL; ++i) h[0][r][i] = start[r][i];
-#pragma unroll
             for (int k = 0; k < CK - HK; ++k) advance(k, h[0], h[0]);
             float odd[3];   // the odd step's sums over states, folded once
 #pragma unroll
             for (int k0 = CK - HK; k0 >= 0; k0 -= HK) {
-            if (HK < CK && k0 == 0) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int i = 0; i < NL; ++i) h[0][r][i] = start[r][i];
-            }
+            if (k0 == 0) load_start();
             forget_lds();
 #pragma unroll
             for (int k = 0; k < HK; ++k) advance(k0 + k, h[k], h[k + 1]);
@@ -596,15 +605,15 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
                 } else {
                     const float S = fold32(fs, odd[0]), R = fold32(fa, odd[1]) * kLn2;
                     const float oe = sh[wave][0][k + half][own], ogy = sh[wave][2][k + half][own];
-                    const float x = ox[k / 2], ddt = (x * S + R) * osv[k / 2];
+                    const float x = sh[wave][3][k + half][own], ddt = (x * S + R) * sh[wave][4][k + half][own];
                     dD += ogy * x;
                     dtbs += ddt;
                     float dz = 0.f;
-                    if (GATE) dz = ozf[k / 2] * fmaf(dskip, x, fold32(fy, odd[2]));
+                    if (GATE) dz = sh[wave][GATE ? 5 : 0][k + half][own] * fmaf(dskip, x, fold32(fy, odd[2]));
                     if (k + half < tn && live) {   // 0 past the sequence's end: e, u, gy, x are
-                        *rx.at(DX, tc + k, d, half) = out_f<T>(fmaf(ogy, dskip, oe * S));
-                        *rt.at(DDT, tc + k, d, half) = out_f<T>(ddt);
-                        if (GATE) *rz.at(DZ, tc + k, d, half) = out_f<T>(dz);
+                        *rx.at(DX, tc + k) = out_f<T>(fmaf(ogy, dskip, oe * S));
+                        *rt.at(DDT, tc + k) = out_f<T>(ddt);
+                        if (GATE) *rz.at(DZ, tc + k) = out_f<T>(dz);
                     }
                 }
             }
@@ -612,9 +621,9 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
         } else if (live) {
             for (int k = 0; k < tn; k += 2) {
                 if (k + half >= tn) continue;
-                *rx.at(DX, tc + k, d, half) = out_f<T>(0.f);
-                *rt.at(DDT, tc + k, d, half) = out_f<T>(0.f);
-                if (GATE) *rz.at(DZ, tc + k, d, half) = out_f<T>(0.f);
+                *rx.at(DX, tc + k) = out_f<T>(0.f);
+                *rt.at(DDT, tc + k) = out_f<T>(0.f);
+                if (GATE) *rz.at(DZ, tc + k) = out_f<T>(0.f);
             }
         }
         __syncthreads();
@@ -651,15 +660,23 @@ __global__ __launch_bounds__(64 * kBwdWaves, MW) void scan_bwd_kernel(ScanArgs a
     }
 }
 
-// dA, dDskip, ddt_bias: the parts summed in their order
-__global__ __launch_bounds__(64) void scan_param_kernel(const float* dA_part, const float* dv_part, int parts, int D,
-                                                        int N, float* dA, float* dD, float* ddtb) {
-    const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, na = int64_t(D) * N;
-    if (i >= na + 2 * D) return;
+// dA, dDskip, ddt_bias: 64 values a workgroup, each wave sums every 16th part,
+// then the waves' sums in their order.
+__global__ __launch_bounds__(1024) void scan_param_kernel(const float* dA_part, const float* dv_part, int parts, int D,
+                                                          int N, float* dA, float* dD, float* ddtb) {
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t i = int64_t(blockIdx.x) * 64 + lane, na = int64_t(D) * N;
+    const bool on = i < na + 2 * D;
     const float* p = i < na ? dA_part + i : dv_part + (i - na);
     const int64_t step = i < na ? na : 2 * int64_t(D);
     float v = 0.f;
-    for (int k = 0; k < parts; ++k) v += p[k * step];
+    if (on)
+        for (int k = wave; k < parts; k += 16) v += p[k * step];
+    red[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0 || !on) return;
+    for (int w = 1; w < 16; ++w) v += red[w][lane];
     if (i < na) dA[i] = v;
     else if (i < na + D) {
         if (dD) dD[i - na] = v;
@@ -882,7 +899,7 @@ janus_status scan_bwd_run(const ScanArgs& a, const int32_t* lengths, float* dA, 
     {
         const int parts = a.nseg * a.B;
         TraceScope trace("scan_param", double(np) * parts, 4.0 * np * parts, st);
-        hipLaunchKernelGGL(scan_param_kernel, dim3((np + 63) / 64), dim3(64), 0, st, a.dA_part, a.dv_part, parts, a.D,
+        hipLaunchKernelGGL(scan_param_kernel, dim3((np + 63) / 64), dim3(1024), 0, st, a.dA_part, a.dv_part, parts, a.D,
                            a.N, dA, dDskip, ddt_bias);
         JANUS_LAUNCH_CHECK();
     }

@@ -10,13 +10,16 @@
 
 namespace janus {
 
-// The lengths of up to kSlice sequences as a kernel argument: no upload, no
+// Up to kSlice sequences and their lengths as a kernel argument: no upload, no
 // device buffer, and a captured launch keeps its own copy.  Larger batches
-// take one launch per slice.
+// take one launch per slice.  The longest come first: workgroups start in that
+// order, and a short sequence at the end leaves less of the chip idle than a
+// long one.
 constexpr int kSlice = 256;
 struct SeqSlice {
     int32_t b0;               // first sequence of the slice
     int32_t len[kSlice];
+    uint8_t at[kSlice];       // entry i is sequence b0 + at[i]
 };
 
 inline janus_status check_lengths(int32_t B, int32_t T, const int32_t* lengths) {
@@ -30,7 +33,9 @@ inline janus_status check_lengths(int32_t B, int32_t T, const int32_t* lengths) 
 inline int fill_slice(SeqSlice& s, int32_t b0, int32_t B, int32_t T, const int32_t* lengths) {
     const int n = std::min(kSlice, B - b0);
     s.b0 = b0;
-    for (int i = 0; i < n; ++i) s.len[i] = lengths ? lengths[b0 + i] : T;
+    for (int i = 0; i < n; ++i) s.at[i] = uint8_t(i);
+    if (lengths) std::stable_sort(s.at, s.at + n, [&](uint8_t i, uint8_t j) { return lengths[b0 + i] > lengths[b0 + j]; });
+    for (int i = 0; i < n; ++i) s.len[i] = lengths ? lengths[b0 + s.at[i]] : T;
     return n;
 }
 
