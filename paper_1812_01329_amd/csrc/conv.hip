@@ -81,7 +81,7 @@ template <typename T, int K, int VEC>
 __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a, SeqSlice s) {
     const int d = (blockIdx.x * blockDim.x + threadIdx.x) * VEC;
     if (d >= a.D) return;
-    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y];
+    const int len = s.len[blockIdx.y], b = seq_of(s, blockIdx.y);
     const int t0 = blockIdx.z * a.seg, t1 = min(a.T, t0 + a.seg), te = min(t1, len);
     float w[K][VEC], bias[VEC], win[K][VEC];   // win[k]: input of time t - K + 1 + k
     load_taps<T, K, VEC>(a, d, w, bias);

@@ -128,7 +128,7 @@ struct Rows {
 // the eight before are worked on.  LOCAL: only the state at the segment's end
 // from a zero start, and the sum of e.
 template <typename T, int NP, bool LOCAL>
-__global__ __launch_bounds__(256, NP <= 16 ? 4 : 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
+__global__ __launch_bounds__(256, 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s) {
     constexpr int CK = chunk_steps(NP), U = NP >= 64 ? 4 : 8;
     __shared__ float bc[kStage * 2 * NP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256, NP <= 16 ? 4 : 2) void scan_fwd_kernel(ScanArg
     const int ch = tile * 64 + lane;
     const bool live = ch < a.Dg;
     const uint32_t d = group * a.Dg + (live ? ch : 0);
-    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y], seg = blockIdx.z;
+    const int len = s.len[blockIdx.y], b = seq_of(s, blockIdx.y), seg = blockIdx.z;
     const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg), te = min(t1, len);
     float A2[NP], h[NP];
 #pragma unroll
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256) void scan_rev_kernel(ScanArgs a, SeqSlice s) {
     const int ch = tile * 64 + lane;
     const bool live = ch < a.Dg;
     const int d = group * a.Dg + (live ? ch : 0);
-    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y], seg = blockIdx.z;
+    const int len = s.len[blockIdx.y], b = seq_of(s, blockIdx.y), seg = blockIdx.z;
     const int t0 = seg * a.seg, te = min(min(a.T, t0 + a.seg), len);
     float A2[NP], g[NP];
 #pragma unroll
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(64 * kBwdWaves, NP <= 16 ? 4 : NP == 32 ? 2 : 1) vo
     const int own = 2 * c16 + (ng & 1), half = ng >> 1;
     const bool live = ch0 + own < a.Dg;
     const uint32_t d = group * a.Dg + (live ? ch0 + own : 0);
-    const int len = s.len[blockIdx.y], b = s.b0 + s.at[blockIdx.y], seg = blockIdx.z;
+    const int len = s.len[blockIdx.y], b = seq_of(s, blockIdx.y), seg = blockIdx.z;
     const int t0 = seg * a.seg, t1 = min(a.T, t0 + a.seg), lim = min(len, t1);
     float A2[2][NL], g[2][NL], dA[2][NL];
     // the lane's channels in the state layout: d2 + r for r < n2

@@ -22,6 +22,11 @@ struct SeqSlice {
     uint8_t at[kSlice];       // entry i is sequence b0 + at[i]
 };
 
+// The sequence of entry i (a byte comes through a vector register: made uniform again)
+__device__ __forceinline__ int seq_of(const SeqSlice& s, int i) {
+    return s.b0 + __builtin_amdgcn_readfirstlane(int(s.at[i]));
+}
+
 inline janus_status check_lengths(int32_t B, int32_t T, const int32_t* lengths) {
     if (lengths)
         for (int32_t b = 0; b < B; ++b)
