@@ -1,17 +1,18 @@
 // Clipped policy loss from logits: rows' log-probabilities and entropies, the
 // loss with its KL and entropy terms, and the gradient of the logits.
 //
-//   M = max x,  S = sum exp(x - M),  E = sum exp(x - M)(x - M)
-//   l = x[a] - M - log S,   H = log S - E / S,   p_j = exp(x_j - M) / S
+//   M = max x,  t = (x - M) log2(e),  S = sum 2^t,  E = sum t 2^t
+//   l = (t[a] - log2 S) ln 2,   H = (log2 S - E / S) ln 2,   p_j = 2^t_j / S
 //   row  = -min(r adv, clip(r) adv) + beta (exp(u) - 1 - u) - eta H,   r = exp(l - old), u = ref - l
 //   c    = d row / d l = -r adv [r adv <= clip(r) adv] - beta (exp(u) - 1)
 //   dx_j = w / W (c (1[j = a] - p_j) + eta p_j (log p_j + H)),   W = sum w
 //
-// One workgroup a row, which it holds in registers between the sums and the
+// One workgroup a row, which it holds in registers from the maximum to the
 // gradient, so the logits are read once and the gradient written once; rows
-// past 64K float32 or 128K bf16 are read twice.  Sums are float32 (float64 over
+// past 64K float32 or 128K bf16 are read three times.  Sums are float32 (float64 over
 // the rows) in a fixed order.
 #include <cmath>
+#include <type_traits>
 
 #include "seq.hpp"
 
@@ -29,7 +30,8 @@ struct PolicyArgs {
     const float *old_logp, *adv, *ref, *weights;
     void* dlogits;        // NULL: scoring
     float *logp, *entropy;
-    const float* W;       // sum of the weights that count
+    float* W;             // sum of the weights that count
+    bool own_W;           // the rows' workgroups form it
     float4* terms;        // [rows] weighted first term, KL, H, clipped
     float lo, hi, beta, eta;
 };
@@ -49,8 +51,6 @@ __device__ __forceinline__ double wsum(double v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
-
-__device__ __forceinline__ float exp_(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 
 // A product that stays rounded: contracted into the sum it goes into, c w / W
 // would leave its rounding error where the gradient is 0 (p = 1 at the action)
@@ -125,33 +125,22 @@ struct Row {
     }
 };
 
-// M, S, E of values seen so far; values join by pieces
+// S = sum 2^t and E = sum t 2^t
 struct Soft {
-    float m = -INFINITY, s = 0.f, e = 0.f;
-    __device__ __forceinline__ void add(float t) {   // t = x - m
-        const float v = exp_(t);
+    float s = 0.f, e = 0.f;
+    __device__ __forceinline__ void add(float t) {
+        const float v = __builtin_amdgcn_exp2f(t);
         s += v;
-        e = fmaf(v, fmaxf(t, kFarBelow), e);
-    }
-    // to a maximum of at least m
-    __device__ __forceinline__ void rescale(float to) {
-        if (m == to || m == -INFINITY) {
-            m = to;
-            return;
-        }
-        const float t = m - to, f = exp_(t);
-        e = f * fmaf(s, fmaxf(t, kFarBelow), e);
-        s *= f;
-        m = to;
+        e = fmaf(v, fmaxf(t, kFarBelow), e);   // (0 * -inf for a forbidden action)
     }
 };
 
-// PIECES 16-byte pieces of the row a thread holds; 0: the row is read again for
-// the gradient.
+// One workgroup a row.  PIECES 16-byte pieces of the row a thread holds; 0: the row is
+// read three times (for its maximum, the sums, the gradient).
 template <typename T, int PIECES, int THREADS>
-__global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a) {
+__global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
     constexpr int VEC = 16 / sizeof(T), WAVES = THREADS / 64;
-    __shared__ float red[3][WAVES];
+    __shared__ float red[4][WAVES];
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool score = !a.dlogits;
     const int act = a.actions[r];
@@ -166,21 +155,24 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a) {
         out = p - row.lo;
     }
     auto no_gradient = [&] {
+        if (score) return;
         if (tid == 0) a.terms[r] = make_float4(0.f, 0.f, 0.f, 0.f);
         const float zero[VEC] = {};
         for (int p = tid; p < np; p += THREADS) row.store(out, same, p, zero);
     };
+    auto answer = [&](float l, float H) {
+        if (tid == 0 && a.logp) a.logp[r] = l;
+        if (tid == 0 && a.entropy) a.entropy[r] = H;
+    };
     if (act < 0 || (w == 0.f && !a.logp && !a.entropy)) {
-        if (tid == 0 && a.logp) a.logp[r] = 0.f;
-        if (tid == 0 && a.entropy) a.entropy[r] = 0.f;
-        if (!score) no_gradient();
+        answer(0.f, 0.f);
+        no_gradient();
         return;
     }
     const float xa = act < a.V ? to_f(static_cast<const T*>(a.logits)[r * a.ld + act]) : NAN;
 
+    // the row, a piece at a time: from registers, or from memory again
     Piece<T> x[PIECES ? PIECES : 1];
-    Soft f;
-    bool nan = false;
     if constexpr (PIECES > 0) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -192,66 +184,78 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a) {
                 for (int j = 0; j < VEC; ++j) x[i].set(j, out_f<T>(-INFINITY));
             }
         }
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) f.m = fmaxf(f.m, x[i].get(j));
-        f.m = wmax(f.m);
-        if (lane == 0) red[0][wave] = f.m;
-        __syncthreads();
-        f.m = red[0][0];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) f.m = fmaxf(f.m, red[0][i]);
-        if (f.m == -INFINITY) {
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) nan = nan || x[i].get(j) != x[i].get(j);
-        } else {
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) f.add(x[i].get(j) - f.m);
-        }
-    } else {
-        for (int p = tid; p < np; p += THREADS) {
-            const Piece<T> v = row.load(p);
-            float m = f.m;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                m = fmaxf(m, v.get(j));
-                nan = nan || v.get(j) != v.get(j);
-            }
-            f.rescale(m);
-            if (m != -INFINITY) {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) f.add(v.get(j) - m);
-            }
-        }
-        float m = wmax(f.m);
-        if (lane == 0) red[0][wave] = m;
-        __syncthreads();
-        m = red[0][0];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) m = fmaxf(m, red[0][i]);
-        f.rescale(m);
     }
-    const bool any_nan = (PIECES == 0 || f.m == -INFINITY) && __syncthreads_or(nan);
+    auto each = [&](auto f) {
+        if constexpr (PIECES > 0) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                // (converted again in each pass: the compiler would hold the row as float32)
+                asm volatile("" : "+v"(x[i].v.x), "+v"(x[i].v.y), "+v"(x[i].v.z), "+v"(x[i].v.w));
+                f(x[i], tid + i * THREADS);
+            }
+        } else {
+            for (int p = tid; p < np; p += THREADS) f(row.load(p), p);
+        }
+    };
+    float m = -INFINITY, W = 0.f;
+    if (!score) {
+        if (a.own_W) {   // few rows: every workgroup adds the weights up, in the same order
+            for (int i = tid; i < a.rows; i += THREADS)
+                if (a.actions[i] >= 0) W += a.weights ? a.weights[i] : 1.f;
+            W = wsum(W);
+            if (lane == 0) red[3][wave] = W;
+        }
+    }
+    each([&](const Piece<T>& v, int) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) m = fmaxf(m, v.get(j));
+    });
+    m = wmax(m);
+    if (lane == 0) red[0][wave] = m;
+    __syncthreads();
+    m = red[0][0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) m = fmaxf(m, red[0][i]);
+    if (!score) {
+        if (a.own_W) {
+            W = 0.f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) W += red[3][i];
+        } else {
+            W = *a.W;
+        }
+    }
+    bool bad = act >= a.V;
+    if (m == -INFINITY) {   // nothing to choose from, or NaN and -inf
+        bool nan = false;
+        each([&](const Piece<T>& v, int) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) nan = nan || v.get(j) != v.get(j);
+        });
+        bad = __syncthreads_or(nan) || bad;
+        if (!bad) {
+            answer(-INFINITY, 0.f);
+            no_gradient();
+            return;
+        }
+    }
+    // (x - M first: the action's own exponent is then exactly 0 where it is the maximum)
+    auto exponent = [&](float v) { return (v - m) * kLog2e; };
+    Soft f;
+    each([&](const Piece<T>& v, int) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) f.add(exponent(v.get(j)));
+    });
     const float s1 = wsum(f.s), e1 = wsum(f.e);
     if (lane == 0) red[1][wave] = s1, red[2][wave] = e1;
     __syncthreads();
     float S = 0.f, E = 0.f;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) S += red[1][i], E += red[2][i];
-    const float M = f.m, logS = __builtin_amdgcn_logf(S) * kLn2, inv = 1.f / S;
-    const bool dead = M == -INFINITY && !any_nan && act < a.V;   // nothing to choose from
-    float l = xa - M - logS, H = logS - E * inv;
-    if (dead) l = -INFINITY, H = 0.f;
-    if (any_nan || act >= a.V) l = NAN, H = NAN;
-    if (tid == 0) {
-        if (a.logp) a.logp[r] = l;
-        if (a.entropy) a.entropy[r] = H;
-    }
+    const float L2 = __builtin_amdgcn_logf(S), inv = 1.f / S;
+    float l = (exponent(xa) - L2) * kLn2, H = (L2 - E * inv) * kLn2;
+    if (bad) l = H = NAN;
+    answer(l, H);
     if (score) return;
     if (w == 0.f) {
         no_gradient();
@@ -267,52 +271,54 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a) {
         kl = kl_term(u);
         c -= a.beta * expm1f(u);
     }
-    if (tid == 0)
-        a.terms[r] = dead ? make_float4(0.f, 0.f, 0.f, 0.f)
-                          : make_float4(w * -(off ? cut : free_), w * kl, w * H, off ? w : 0.f);
-    const float scale = w / *a.W, cs = rounded_mul(c, scale), es = a.eta * scale, bad = any_nan || act >= a.V ? NAN : 0.f;
-    const int ai = act < a.V ? row.lo + act : -1;
-    auto grad = [&](const Piece<T>& v, int p) {
+    if (tid == 0) a.terms[r] = make_float4(w * -(off ? cut : free_), w * kl, w * H, off ? w : 0.f);
+    // gradient p (es (log p + H) - cs), and cs more at the action
+    const float scale = w / W, cs = bad ? NAN : rounded_mul(c, scale), es = a.eta * scale;
+    const float g0 = (es * (H - L2 * kLn2) - cs) * inv, g1 = es * kLn2 * inv;
+    const int ai = row.lo + (bad ? 0 : act), ap = ai / VEC;
+    auto grad = [&](const Piece<T>& v, int p, auto entropy) {
+        if (p >= np) return;
         float g[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const float t = v.get(j) - M, pj = exp_(t) * inv;
-            g[j] = -cs * pj;
-            if (es != 0.f) g[j] = fmaf(es * pj, fmaxf(t, kFarBelow) - logS + H, g[j]);
-            if (p * VEC + j == ai) g[j] += cs;
-            g[j] = dead ? 0.f : g[j] + bad;
+            const float t = exponent(v.get(j)), e = __builtin_amdgcn_exp2f(t);
+            g[j] = e * (entropy.value ? fmaf(g1, fmaxf(t, kFarBelow), g0) : g0);
+        }
+        if (p == ap) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (p * VEC + j == ai) g[j] += cs;
         }
         row.store(out, same, p, g);
     };
-    if constexpr (PIECES > 0) {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i)
-            if (tid + i * THREADS < np) grad(x[i], tid + i * THREADS);
-    } else {
-        for (int p = tid; p < np; p += THREADS) grad(row.load(p), p);
-    }
+    if (es != 0.f) each([&](const Piece<T>& v, int p) { grad(v, p, std::true_type{}); });
+    else each([&](const Piece<T>& v, int p) { grad(v, p, std::false_type{}); });
 }
 
-// W, one workgroup
-__global__ __launch_bounds__(1024) void policy_weight_kernel(const int32_t* actions, const float* weights, int rows,
-                                                             float* W) {
-    __shared__ double red[16];
+// The weights that count, added up by one workgroup (the result in thread 0)
+__device__ __forceinline__ double sum_weights(const PolicyArgs& a, double* red) {
     double s = 0.0;
-    for (int r = threadIdx.x; r < rows; r += 1024)
-        if (actions[r] >= 0) s += weights ? weights[r] : 1.f;
+    for (int r = threadIdx.x; r < a.rows; r += 1024)
+        if (a.actions[r] >= 0) s += a.weights ? a.weights[r] : 1.f;
     s = wsum(s);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        double t = 0.0;
+    double t = 0.0;
+    if (threadIdx.x == 0)
         for (int i = 0; i < 16; ++i) t += red[i];
-        *W = float(t);
-    }
+    return t;
+}
+
+__global__ __launch_bounds__(1024) void policy_weight_kernel(PolicyArgs a) {
+    __shared__ double red[16];
+    const double t = sum_weights(a, red);
+    if (threadIdx.x == 0) *a.W = float(t);
 }
 
 // the statistics, one workgroup
 __global__ __launch_bounds__(1024) void policy_stats_kernel(PolicyArgs a, float* stats) {
-    __shared__ double red[4][16];
+    __shared__ double red[5][16];
+    const double own = a.own_W ? sum_weights(a, red[4]) : 0.0;
     double s[4] = {};
     for (int r = threadIdx.x; r < a.rows; r += 1024) {
         const float4 t = a.terms[r];
@@ -325,7 +331,7 @@ __global__ __launch_bounds__(1024) void policy_stats_kernel(PolicyArgs a, float*
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        const double W = *a.W;
+        const double W = a.own_W ? own : *a.W;
         for (int k = 0; k < 4; ++k) {
             s[k] = 0.0;
             for (int i = 0; i < 16; ++i) s[k] += red[k][i];
@@ -342,19 +348,23 @@ bool policy_desc_ok(const janus_policy_desc* d) {
            d->clip_low >= 0.f && std::isfinite(d->clip_high) && d->clip_high >= 0.f && std::isfinite(d->kl_coef) &&
            std::isfinite(d->ent_coef);
 }
-size_t policy_carve(PolicyArgs& a, float** W, int rows, void* ws) {
+size_t policy_carve(PolicyArgs& a, int rows, void* ws) {
     Carver c(ws);
-    *W = c.take<float>(1);
-    a.W = *W;
+    a.W = c.take<float>(1);
     a.terms = c.take<float4>(rows);
     return c.off;
 }
+
+// Up to this many rows each workgroup adds the weights up itself: a launch less.
+constexpr int kOwnWeightRows = 2048;
 
 template <typename T, int PIECES, int THREADS>
 void row_launch(const PolicyArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((policy_row_kernel<T, PIECES, THREADS>), dim3(a.rows), dim3(THREADS), 0, st, a);
 }
-// The fewest pieces a thread that hold a row (which may touch one piece more than its length fills)
+// The fewest pieces a thread that hold a row (which may touch one piece more
+// than its length fills): small workgroups as long as 16 pieces do, since
+// several of them on a CU load, sum and store at different times.
 template <typename T>
 void row_dispatch(const PolicyArgs& a, hipStream_t st) {
     const int64_t np = (int64_t(a.V) + 16 / sizeof(T) - 2) / (16 / sizeof(T)) + 1;
@@ -362,8 +372,8 @@ void row_dispatch(const PolicyArgs& a, hipStream_t st) {
     else if (np <= 512) row_launch<T, 2, 256>(a, st);
     else if (np <= 1024) row_launch<T, 4, 256>(a, st);
     else if (np <= 2048) row_launch<T, 8, 256>(a, st);
-    else if (np <= 4096) row_launch<T, 4, 1024>(a, st);
-    else if (np <= 8192) row_launch<T, 8, 1024>(a, st);
+    else if (np <= 4096 + 1) row_launch<T, 17, 256>(a, st);
+    else if (np <= 8192) row_launch<T, 16, 512>(a, st);
     else if (np <= 16384) row_launch<T, 16, 1024>(a, st);
     else row_launch<T, 0, 1024>(a, st);
 }
@@ -376,8 +386,7 @@ using namespace janus;
 extern "C" size_t janus_policy_workspace_bytes(const janus_policy_desc* d) {
     if (!policy_desc_ok(d) || !dtype_ok(d->dtype)) return 0;
     PolicyArgs a{};
-    float* W;
-    return policy_carve(a, &W, d->rows, nullptr);
+    return policy_carve(a, d->rows, nullptr);
 }
 
 extern "C" janus_status janus_policy_loss(const janus_policy_desc* d, const void* logits, const int32_t* actions,
@@ -394,8 +403,7 @@ extern "C" janus_status janus_policy_loss(const janus_policy_desc* d, const void
                            static_cast<const float*>(entropy), static_cast<const float*>(stats)})
         if (!aligned(p, 4)) return JANUS_ERR_INVALID_ARG;
     PolicyArgs a{};
-    float* W;
-    const size_t need = policy_carve(a, &W, d->rows, ws);
+    const size_t need = policy_carve(a, d->rows, ws);
     if (!score && (!ws || ws_bytes < need || !aligned(ws, 256))) return JANUS_ERR_WORKSPACE;
     a.rows = d->rows, a.V = d->V, a.ld = d->ld ? d->ld : d->V;
     a.logits = logits, a.actions = actions, a.old_logp = old_logp, a.adv = adv, a.ref = ref_logp, a.weights = weights;
@@ -403,9 +411,10 @@ extern "C" janus_status janus_policy_loss(const janus_policy_desc* d, const void
     a.lo = d->clip_low, a.hi = d->clip_high, a.beta = d->kl_coef, a.eta = d->ent_coef;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const double el = double(d->rows) * d->V;
-    if (!score) {
+    a.own_W = d->rows <= kOwnWeightRows;
+    if (!score && !a.own_W) {
         TraceScope trace("policy_weight", double(d->rows), 8.0 * d->rows, st);
-        hipLaunchKernelGGL(policy_weight_kernel, dim3(1), dim3(1024), 0, st, actions, weights, d->rows, W);
+        hipLaunchKernelGGL(policy_weight_kernel, dim3(1), dim3(1024), 0, st, a);
         JANUS_LAUNCH_CHECK();
     }
     {
