@@ -135,6 +135,38 @@ struct Soft {
     }
 };
 
+// A thread's share of the weights that count, eight rows' loads at once
+template <int THREADS, typename S>
+__device__ __forceinline__ S part_of_weights(const PolicyArgs& a) {
+    constexpr int U = 8;
+    S s = 0;
+    for (int r0 = threadIdx.x; r0 < a.rows; r0 += U * THREADS) {
+        int act[U];
+        float w[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int r = min(r0 + i * THREADS, a.rows - 1);
+            act[i] = a.actions[r];
+            w[i] = a.weights ? a.weights[r] : 1.f;
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (r0 + i * THREADS < a.rows && act[i] >= 0) s += w[i];
+    }
+    return s;
+}
+
+// The weights that count, added up by one workgroup (the result in thread 0)
+__device__ __forceinline__ double sum_weights(const PolicyArgs& a, double* red) {
+    const double s = wsum(part_of_weights<1024, double>(a));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    double t = 0.0;
+    if (threadIdx.x == 0)
+        for (int i = 0; i < 16; ++i) t += red[i];
+    return t;
+}
+
 // One workgroup a row.  PIECES 16-byte pieces of the row a thread holds; 0: the row is
 // read three times (for its maximum, the sums, the gradient).
 template <typename T, int PIECES, int THREADS>
@@ -169,20 +201,36 @@ __global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
         no_gradient();
         return;
     }
+    float old = 0.f, adv = 0.f, ref = 0.f;   // (on their way with the row)
+    if (!score) {
+        old = a.old_logp[r], adv = a.adv[r];
+        if (a.ref) ref = a.ref[r];
+    }
     const float xa = act < a.V ? to_f(static_cast<const T*>(a.logits)[r * a.ld + act]) : NAN;
 
     // the row, a piece at a time: from registers, or from memory again
-    Piece<T> x[PIECES ? PIECES : 1];
+    Piece<T> x[PIECES ? PIECES : 1], none;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) none.set(j, out_f<T>(-INFINITY));
     if constexpr (PIECES > 0) {
+        // (rows of whole pieces: loads without a branch between them go out together)
+        if (row.lo == 0 && row.hi % VEC == 0) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                x[i].v = reinterpret_cast<const uint4*>(row.base)[min(tid + i * THREADS, np - 1)];
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if (tid + i * THREADS >= np) x[i] = none;
+        } else {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int p = tid + i * THREADS;
             if (p < np) {
                 x[i] = row.load(p);
             } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) x[i].set(j, out_f<T>(-INFINITY));
+                x[i] = none;
             }
+        }
         }
     }
     auto each = [&](auto f) {
@@ -200,9 +248,7 @@ __global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
     float m = -INFINITY, W = 0.f;
     if (!score) {
         if (a.own_W) {   // few rows: every workgroup adds the weights up, in the same order
-            for (int i = tid; i < a.rows; i += THREADS)
-                if (a.actions[i] >= 0) W += a.weights ? a.weights[i] : 1.f;
-            W = wsum(W);
+            W = wsum(part_of_weights<THREADS, float>(a));
             if (lane == 0) red[3][wave] = W;
         }
     }
@@ -262,12 +308,12 @@ __global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
         return;
     }
 
-    const float ratio = expf(l - a.old_logp[r]), adv = a.adv[r];
+    const float ratio = expf(l - old);
     const float free_ = ratio * adv, cut = fminf(fmaxf(ratio, 1.f - a.lo), 1.f + a.hi) * adv;
     const bool off = free_ > cut;
     float c = off ? 0.f : -free_, kl = 0.f;
     if (a.ref) {
-        const float u = a.ref[r] - l;
+        const float u = ref - l;
         kl = kl_term(u);
         c -= a.beta * expm1f(u);
     }
@@ -295,20 +341,6 @@ __global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
     else each([&](const Piece<T>& v, int p) { grad(v, p, std::false_type{}); });
 }
 
-// The weights that count, added up by one workgroup (the result in thread 0)
-__device__ __forceinline__ double sum_weights(const PolicyArgs& a, double* red) {
-    double s = 0.0;
-    for (int r = threadIdx.x; r < a.rows; r += 1024)
-        if (a.actions[r] >= 0) s += a.weights ? a.weights[r] : 1.f;
-    s = wsum(s);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-    __syncthreads();
-    double t = 0.0;
-    if (threadIdx.x == 0)
-        for (int i = 0; i < 16; ++i) t += red[i];
-    return t;
-}
-
 __global__ __launch_bounds__(1024) void policy_weight_kernel(PolicyArgs a) {
     __shared__ double red[16];
     const double t = sum_weights(a, red);
@@ -320,9 +352,14 @@ __global__ __launch_bounds__(1024) void policy_stats_kernel(PolicyArgs a, float*
     __shared__ double red[5][16];
     const double own = a.own_W ? sum_weights(a, red[4]) : 0.0;
     double s[4] = {};
-    for (int r = threadIdx.x; r < a.rows; r += 1024) {
-        const float4 t = a.terms[r];
-        s[0] += t.x, s[1] += t.y, s[2] += t.z, s[3] += t.w;
+    constexpr int U = 8;
+    for (int r0 = threadIdx.x; r0 < a.rows; r0 += U * 1024) {
+        float4 t[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) t[i] = a.terms[min(r0 + i * 1024, a.rows - 1)];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (r0 + i * 1024 < a.rows) s[0] += t[i].x, s[1] += t[i].y, s[2] += t[i].z, s[3] += t[i].w;
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -363,18 +400,22 @@ void row_launch(const PolicyArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((policy_row_kernel<T, PIECES, THREADS>), dim3(a.rows), dim3(THREADS), 0, st, a);
 }
 // The fewest pieces a thread that hold a row (which may touch one piece more
-// than its length fills): small workgroups as long as 16 pieces do, since
-// several of them on a CU load, sum and store at different times.
+// than its length fills), since every pass works on all of them: small
+// workgroups as long as 17 pieces do, for several of them on a CU load, sum and
+// store at different times.
+template <typename T, int P, int... MORE>
+void row_small(int64_t np, const PolicyArgs& a, hipStream_t st) {
+    if (np <= 256 * P) return row_launch<T, P, 256>(a, st);
+    if constexpr (sizeof...(MORE) > 0) row_small<T, MORE...>(np, a, st);
+}
 template <typename T>
 void row_dispatch(const PolicyArgs& a, hipStream_t st) {
     const int64_t np = (int64_t(a.V) + 16 / sizeof(T) - 2) / (16 / sizeof(T)) + 1;
-    if (np <= 256) row_launch<T, 1, 256>(a, st);
-    else if (np <= 512) row_launch<T, 2, 256>(a, st);
-    else if (np <= 1024) row_launch<T, 4, 256>(a, st);
-    else if (np <= 2048) row_launch<T, 8, 256>(a, st);
-    else if (np <= 4096 + 1) row_launch<T, 17, 256>(a, st);
-    else if (np <= 8192) row_launch<T, 16, 512>(a, st);
-    else if (np <= 16384) row_launch<T, 16, 1024>(a, st);
+    if (np <= 256 * 17) row_small<T, 1, 2, 3, 4, 5, 6, 8, 10, 13, 17>(np, a, st);
+    else if (np <= 512 * 12) row_launch<T, 12, 512>(a, st);
+    else if (np <= 512 * 16) row_launch<T, 16, 512>(a, st);
+    else if (np <= 1024 * 12) row_launch<T, 12, 1024>(a, st);
+    else if (np <= 1024 * 16) row_launch<T, 16, 1024>(a, st);
     else row_launch<T, 0, 1024>(a, st);
 }
 
@@ -394,7 +435,7 @@ extern "C" janus_status janus_policy_loss(const janus_policy_desc* d, const void
                                           const float* weights, void* dlogits, float* logp, float* entropy,
                                           float* stats, void* ws, size_t ws_bytes, void* stream) {
     if (!policy_desc_ok(d) || !logits || !actions) return JANUS_ERR_INVALID_ARG;
-    if (!dtype_ok(d->dtype) || d->V > (1 << 30)) return JANUS_ERR_UNSUPPORTED;
+    if (!dtype_ok(d->dtype) || d->V > (1 << 30) || d->rows > (1 << 30)) return JANUS_ERR_UNSUPPORTED;
     const bool score = !dlogits;
     if (score ? (old_logp || adv || stats) : (!old_logp || !adv)) return JANUS_ERR_INVALID_ARG;
     const size_t es = dtype_size(d->dtype);
