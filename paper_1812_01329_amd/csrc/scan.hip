@@ -56,6 +56,7 @@ struct ScanArgs {
     float* dv_part;   // [nseg * B][2][D] sums of gy x and of ddt
     float* bc_part;   // [bblocks][T * B][G][2][NP], or NULL with one workgroup a group
     bool softplus;
+    bool bc4;         // (step) four states of B and C are one aligned access
 };
 
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -730,9 +731,19 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, const int32_
         for (int j = 0; j < 4; ++j)
             if (n0 + j < a.N) h[j] = sp[j], A[j] = ap[j];
     }
+    if (VEC4 && a.bc4) {
+        if (n0 < a.N) {
+            Chan<T, 4> rb, rc;
+            rb.load(bp);
+            rc.load(cp);
+            rb.get(bn);
+            rc.get(cn);
+        }
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (n0 + j < a.N) bn[j] = to_f(bp[j]), cn[j] = to_f(cp[j]);
+        for (int j = 0; j < 4; ++j)
+            if (n0 + j < a.N) bn[j] = to_f(bp[j]), cn[j] = to_f(cp[j]);
+    }
     const float x = to_f(static_cast<const T*>(a.x)[b * a.ldx + d]);
     const float e = step_size(to_f(static_cast<const T*>(a.dt)[b * a.ldt + d]) + (a.dtb ? a.dtb[d] : 0.f), a.softplus);
     float y = 0.f;
@@ -1021,6 +1032,8 @@ extern "C" janus_status janus_selective_scan_step(const janus_scan_desc* d, cons
     ScanArgs a = scan_geometry(d);
     scan_inputs(a, x, dt, A, Bm, Cm, Dskip, z, dt_bias);
     a.y = y;
+    const size_t four = 4 * dtype_size(d->dtype);
+    a.bc4 = a.ldb % 4 == 0 && a.ldc % 4 == 0 && aligned(Bm, four) && aligned(Cm, four);
     hipStream_t st = static_cast<hipStream_t>(stream);
     TraceScope trace("scan_step", 7.0 * a.B * a.D * a.N, 8.0 * a.B * a.D * a.N, st);
     return d->dtype == JANUS_BF16 ? with_states<StepRun, bf16_t>(a.N, a, slots, n_slots, state, st)

@@ -215,7 +215,8 @@ def _stream(stream=None) -> Optional[int]:
     if stream is not None:
         return stream
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    # (the handle alone: a torch.cuda.Stream object costs more than the rest of a small call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _ptr_array(tensors: Sequence) -> C.Array:
