@@ -306,44 +306,32 @@ __global__ __launch_bounds__(256) void scan_rev_kernel(ScanArgs a, SeqSlice s) {
 }
 
 // Chains the segments.  forward: seg_h[i] becomes the state at segment i's
-// start; reverse: seg_g[i] becomes what flows into segment i's end.
+// start; reverse: seg_g[i] becomes what flows into segment i's end.  A lane has
+// one state; the loads of 16 segments go out together.
 template <int NP, bool REVERSE>
 __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
-    const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;   // (b, quarter, d)
-    if (i >= int64_t(a.B) * (NP / 4) * a.D) return;
-    const int d = int(i % a.D), q = int(i / a.D % (NP / 4)), b = int(i / a.D / (NP / 4));
+    const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, size = int64_t(a.B) * NP * a.D;   // [B][NP / 4][D][4]
+    if (i >= size) return;
+    const int d = int(i / 4 % a.D), b = int(i / 4 / a.D / (NP / 4)), n = int(i / 4 / a.D % (NP / 4)) * 4 + int(i % 4);
     const float* first = REVERSE ? a.dhT : a.h0;
-    float A2[4], h[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = 4 * q + j;
-        A2[j] = n < a.N ? a.A[int64_t(d) * a.N + n] * kLog2e : 0.f;
-        h[j] = n < a.N && first ? first[(int64_t(b) * a.D + d) * a.N + n] : 0.f;
-    }
-    constexpr int U = 8;   // segments whose loads go out together
+    const float A2 = n < a.N ? a.A[int64_t(d) * a.N + n] * kLog2e : 0.f;
+    float h = n < a.N && first ? first[(int64_t(b) * a.D + d) * a.N + n] : 0.f;
+    float* const p = (REVERSE ? a.seg_g : a.seg_h) + i;
+    const float* const ep = a.seg_e + int64_t(b) * a.D + d;
+    constexpr int U = 16;
     for (int k0 = 0; k0 < a.nseg; k0 += U) {
-        float4 v[U];
-        float e[U];
-        auto at = [&](int k) {
-            return reinterpret_cast<float4*>(
-                state_at<NP>(REVERSE ? a.seg_g : a.seg_h, a, REVERSE ? a.nseg - 1 - k : k, b, q, d));
-        };
+        float v[U], e[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k)
-            if (k0 + k < a.nseg - 1) {   // (nothing flows out of the last one)
-                v[k] = *at(k0 + k);
-                e[k] = a.seg_e[(int64_t(REVERSE ? a.nseg - 1 - k0 - k : k0 + k) * a.B + b) * a.D + d];
-            }
+        for (int k = 0; k < U; ++k) {
+            const int seg = REVERSE ? max(a.nseg - 1 - k0 - k, 0) : min(k0 + k, a.nseg - 1);
+            v[k] = p[seg * size];
+            e[k] = ep[int64_t(seg) * a.B * a.D];
+        }
 #pragma unroll
         for (int k = 0; k < U; ++k)
             if (k0 + k < a.nseg) {
-                *at(k0 + k) = make_float4(h[0], h[1], h[2], h[3]);
-                if (k0 + k < a.nseg - 1) {
-                    h[0] = fmaf(exp2_(e[k] * A2[0]), h[0], v[k].x);
-                    h[1] = fmaf(exp2_(e[k] * A2[1]), h[1], v[k].y);
-                    h[2] = fmaf(exp2_(e[k] * A2[2]), h[2], v[k].z);
-                    h[3] = fmaf(exp2_(e[k] * A2[3]), h[3], v[k].w);
-                }
+                p[(REVERSE ? a.nseg - 1 - k0 - k : k0 + k) * size] = h;
+                h = fmaf(exp2_(e[k] * A2), h, v[k]);   // (past the last segment it is not used)
             }
     }
 }
@@ -806,10 +794,11 @@ ScanArgs scan_geometry(const janus_scan_desc* d) {
     a.btiles = (a.Dg + 31) / 32;
     a.bblocks = (a.btiles + kBwdWaves - 1) / kBwdWaves;
     // With fewer waves than the chip's 1024 SIMDs the time axis is cut, into segments of 64 steps
-    // and more, for two waves a SIMD: the cut costs a second pass over the inputs.
+    // and more, for four waves a SIMD.  The cut costs a second pass over the inputs: one prompt of
+    // 8192 steps and 2048 channels takes 32 waves 4.1 ms in one piece, 0.17 ms in 128.
     const int64_t waves = int64_t(a.B) * a.G * a.tiles;
     int64_t want = 1;
-    if (waves < 1024) want = std::max<int64_t>(1, std::min<int64_t>((2048 + waves - 1) / waves, a.T / 64));
+    if (waves < 1024) want = std::max<int64_t>(1, std::min<int64_t>((4096 + waves - 1) / waves, a.T / 64));
     a.seg = int(std::max<int64_t>(kStage, round_up((a.T + want - 1) / want, kStage)));
     a.nseg = std::max(1, (a.T + a.seg - 1) / a.seg);
     return a;
@@ -865,8 +854,8 @@ janus_status scan_fwd_run(const ScanArgs& a, const int32_t* lengths, hipStream_t
                                s);
             JANUS_LAUNCH_CHECK();
         }
-        const int64_t all = int64_t(a.B) * (NP / 4) * a.D;
-        TraceScope trace("scan_chain", 8.0 * all * a.nseg, 36.0 * all * a.nseg, st);
+        const int64_t all = int64_t(a.B) * NP * a.D;
+        TraceScope trace("scan_chain", 2.0 * all * a.nseg, 9.0 * all * a.nseg, st);
         hipLaunchKernelGGL((scan_chain_kernel<NP, false>), dim3((all + 255) / 256), dim3(256), 0, st, a);
         JANUS_LAUNCH_CHECK();
     }
@@ -892,8 +881,8 @@ janus_status scan_bwd_run(const ScanArgs& a, const int32_t* lengths, float* dA, 
             hipLaunchKernelGGL((scan_rev_kernel<T, NP>), dim3(a.blocks * a.G, n, a.nseg), scan_block(a), 0, st, a, s);
             JANUS_LAUNCH_CHECK();
         }
-        const int64_t all = int64_t(a.B) * (NP / 4) * a.D;
-        TraceScope trace("scan_chain", 8.0 * all * a.nseg, 36.0 * all * a.nseg, st);
+        const int64_t all = int64_t(a.B) * NP * a.D;
+        TraceScope trace("scan_chain", 2.0 * all * a.nseg, 9.0 * all * a.nseg, st);
         hipLaunchKernelGGL((scan_chain_kernel<NP, true>), dim3((all + 255) / 256), dim3(256), 0, st, a);
         JANUS_LAUNCH_CHECK();
     }
