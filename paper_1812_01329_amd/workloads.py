@@ -413,6 +413,48 @@ def sst_childsum(n_trees=25, E=300, H=150, V=20000, C=5, min_nodes=5, max_nodes=
     return ChildSumWorkload("childsum", E, H, V, C, trees, labels, emb, W, U, b, Ws, bs)
 
 
+# --------------------------------------------------------------------------
+# Sequence policy
+# --------------------------------------------------------------------------
+@dataclasses.dataclass
+class PolicyWorkload:
+    """Inputs of one policy-gradient step over sampled token sequences: the
+    parameters of a selective-scan token model and a batch of rollouts.
+
+    Rows are (t, b); the model reads ``tokens[t]`` and its action is
+    ``tokens[t + 1]`` while t < lengths[b]."""
+    name: str
+    dtype: str
+    V: int
+    M: int                 # embedding width
+    D: int                 # channels of the convolution and the scan
+    N: int                 # states per channel
+    K: int                 # taps of the convolution
+    R: int                 # rank of the step sizes' projection
+    B: int
+    T: int
+    lengths: np.ndarray    # [B] int32
+    tokens: np.ndarray     # [T + 1, B] int32
+    adv: np.ndarray        # [B] float32, one advantage a sequence
+    params: Dict[str, np.ndarray]
+
+
+def sequence_policy(V=1000, M=128, D=256, N=16, K=4, R=8, B=8, T=24, dtype=F32, seed=None) -> PolicyWorkload:
+    """Token policy of one convolution and selective-scan layer: lengths uniform
+    in [1, T], Zipf(1.1) tokens, advantages N(0, 1); products' weights U(-a, a)
+    with a = 1/sqrt(width), decay rates 1..N, step sizes log-uniform in
+    [0.001, 0.1] through the bias."""
+    rp, _, rl, rt = _streams(7, seed)
+    w = lambda *s: _round_if(uniform(rp, 1.0 / np.sqrt(s[-1]), s), dtype)
+    d0 = np.exp(rp.uniform(np.log(1e-3), np.log(1e-1), D))
+    params = dict(E=w(V, M), Win=w(2 * D, M), conv_w=w(D, K), conv_b=w(D), Wx=w(R + 2 * N, D), Wdt=w(D, R),
+                  Wout=w(V, D), A=-np.tile(np.arange(1, N + 1, dtype=np.float32), (D, 1)),
+                  Dskip=np.ones(D, np.float32), dt_bias=(d0 + np.log(-np.expm1(-d0))).astype(np.float32))
+    lengths = rl.integers(1, T + 1, size=B).astype(np.int32)
+    tokens = zipf_truncated(rt, 1.1, V, (T + 1, B))
+    return PolicyWorkload("policy", dtype, V, M, D, N, K, R, B, T, lengths, tokens, normal(rt, (B,)), params)
+
+
 # Named full-size workloads, in the order of the five configurations.
 FULL: Dict[str, callable] = {
     "tiny": tiny_lstm,
