@@ -113,15 +113,21 @@ __device__ __forceinline__ void stage_bc(const ScanArgs& a, float* lds, int t, i
     }
 }
 
-// Rows (t, b) of an operand: a uniform address, to which a lane adds its channel.
-struct Rows {
-    int64_t step, base;    // bytes from row (t, b) to (t + 1, b), of row (0, b)
-    __device__ __forceinline__ Rows(int64_t ld, int B, int b, int es) : step(int64_t(B) * ld * es), base(b * ld * es) {}
-    template <typename T>
-    __device__ __forceinline__ T* at(T* p, int t) const {
-        return reinterpret_cast<T*>(
-            uniform(reinterpret_cast<char*>(const_cast<std::remove_const_t<T>*>(p)) + base + t * step));
-    }
+// A walk over the rows (t, b) of an operand: the row's address is uniform, and a
+// lane adds its channel's byte offset (32 bits).
+template <typename T>
+struct Walk {
+    char* row;
+    int64_t step;
+    uint32_t off;
+    __device__ __forceinline__ Walk(const void* p, int64_t ld, int B, int b, int t, uint32_t d)
+        : row(uniform(static_cast<char*>(const_cast<void*>(p)) + (int64_t(t) * B + b) * ld * int64_t(sizeof(T)))),
+          step(int64_t(B) * ld * int64_t(sizeof(T))), off(d * uint32_t(sizeof(T))) {}
+    __device__ __forceinline__ T get() const { return *reinterpret_cast<const T*>(row + fresh(off)); }
+    __device__ __forceinline__ void put(T v) const { *reinterpret_cast<T*>(row + fresh(off)) = v; }
+    // to the next row, or (at the end of what there is) not
+    __device__ __forceinline__ void on(bool more = true) { row = uniform(row + (more ? step : 0)); }
+    __device__ __forceinline__ void back(bool more = true) { row = uniform(row - (more ? step : 0)); }
 };
 
 // One lane per channel, its NP states in registers; B and C come from LDS, the
@@ -157,20 +163,23 @@ __global__ __launch_bounds__(256, 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s
             if (n < a.N) h[n] = a.h0[(int64_t(b) * a.D + d) * a.N + n];
     }
     const float dskip = a.Dskip ? a.Dskip[d] : 0.f, dtb = a.dtb ? a.dtb[d] : 0.f;
-    const T *X = static_cast<const T*>(a.x), *DT = static_cast<const T*>(a.dt), *Z = static_cast<const T*>(a.z);
-    T* Y = static_cast<T*>(a.y);
-    const Rows rx(a.ldx, a.B, b, sizeof(T)), rt(a.ldt, a.B, b, sizeof(T)), rz(a.ldz, a.B, b, sizeof(T)),
-        ry(a.ldy, a.B, b, sizeof(T));
-    const bool gate = !LOCAL && Z;
+    Walk<T> X(a.x, a.ldx, a.B, b, t0, d), DT(a.dt, a.ldt, a.B, b, t0, d), Z(a.z, a.ldz, a.B, b, t0, d),
+        Y(a.y, a.ldy, a.B, b, t0, d);
+    const bool gate = !LOCAL && a.z;
     float esum = 0.f;
     T nx[U], nt[U], nz[U];   // rows on their way (past the end: the last one again, not used)
     auto fetch = [&](int t) {
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int r = min(t + i, te - 1);
-            nx[i] = rx.at(X, r)[d];
-            nt[i] = rt.at(DT, r)[d];
-            if (gate) nz[i] = rz.at(Z, r)[d];
+            const bool more = t + i + 1 < te;
+            nx[i] = X.get();
+            X.on(more);
+            nt[i] = DT.get();
+            DT.on(more);
+            if (gate) {
+                nz[i] = Z.get();
+                Z.on(more);
+            }
         }
     };
     if (t0 < te) fetch(t0);
@@ -215,11 +224,12 @@ __global__ __launch_bounds__(256, 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s
 #pragma unroll
                     for (int i = 0; i < U; ++i) y[i] *= z[i] * sigmoidf_(z[i]);
                 }
-                if (live) {
 #pragma unroll
-                    for (int i = 0; i < U; ++i)
-                        if (tu + i < te) ry.at(Y, tu + i)[d] = out_f<T>(y[i]);
-                }
+                for (int i = 0; i < U; ++i)
+                    if (tu + i < te) {
+                        if (live) Y.put(out_f<T>(y[i]));
+                        Y.on();
+                    }
             }
         }
     }
@@ -233,7 +243,7 @@ __global__ __launch_bounds__(256, 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s
         a.seg_e[(int64_t(seg) * a.B + b) * a.D + df] = esum;
         return;
     }
-    for (int t = max(t0, len); t < t1; ++t) ry.at(Y, t)[d] = out_f<T>(0.f);
+    for (int t = max(t0, len); t < t1; ++t, Y.on()) Y.put(out_f<T>(0.f));
     if (a.hT && seg == a.nseg - 1) {
 #pragma unroll
         for (int n = 0; n < NP; ++n)
@@ -241,17 +251,17 @@ __global__ __launch_bounds__(256, 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s
     }
 }
 
-// The other direction of LOCAL: G at a segment's start from a zero end,
-// without its own... the part that flows into the segment before it.
+// LOCAL in the other direction: what flows from a segment into the one before
+// it, from a zero end.
 template <typename T, int NP>
-__global__ __launch_bounds__(256) void scan_rev_kernel(ScanArgs a, SeqSlice s) {
-    constexpr int U = 8;
+__global__ __launch_bounds__(256, 2) void scan_rev_kernel(ScanArgs a, SeqSlice s) {
+    constexpr int U = NP >= 64 ? 4 : 8;
     __shared__ float bc[kStage * 2 * NP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int group = blockIdx.x / a.blocks, tile = (blockIdx.x % a.blocks) * waves + wave;
     const int ch = tile * 64 + lane;
     const bool live = ch < a.Dg;
-    const int d = group * a.Dg + (live ? ch : 0);
+    const uint32_t d = group * a.Dg + (live ? ch : 0);
     const int len = s.len[blockIdx.y], b = seq_of(s, blockIdx.y), seg = blockIdx.z;
     const int t0 = seg * a.seg, te = min(min(a.T, t0 + a.seg), len);
     float A2[NP], g[NP];
@@ -261,40 +271,56 @@ __global__ __launch_bounds__(256) void scan_rev_kernel(ScanArgs a, SeqSlice s) {
         g[n] = 0.f;
     }
     const float dtb = a.dtb ? a.dtb[d] : 0.f;
-    const T* tp = static_cast<const T*>(a.dt) + b * a.ldt + d;
-    const T* zp = a.z ? static_cast<const T*>(a.z) + b * a.ldz + d : nullptr;
-    const T* gp = static_cast<const T*>(a.dy) + b * a.ldy + d;
-    const int64_t st = a.B * a.ldt, sz = a.B * a.ldz, sy = a.B * a.ldy;
+    const int last = max(te - 1, 0);
+    Walk<T> DT(a.dt, a.ldt, a.B, b, last, d), Z(a.z, a.ldz, a.B, b, last, d), DY(a.dy, a.ldy, a.B, b, last, d);
+    const bool gate = a.z;
+    T nt[U], nz[U], ng[U];   // rows t - 1, t - 2, ... on their way (before the start: the first one again, not used)
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool more = t - 2 - i >= t0;
+            nt[i] = DT.get();
+            DT.back(more);
+            ng[i] = DY.get();
+            DY.back(more);
+            if (gate) {
+                nz[i] = Z.get();
+                Z.back(more);
+            }
+        }
+    };
+    if (t0 < te) fetch(te);
     const int n_stage = te > t0 ? (te - t0 + kStage - 1) / kStage : 0;
     for (int k = n_stage - 1; k >= 0; --k) {
         const int ts = t0 + k * kStage, tn = min(te, ts + kStage);
         __syncthreads();
-        stage_bc<T, NP>(a, bc, ts, tn - ts, te, b, group);
+        stage_bc<T, NP>(a, bc, ts, kStage, te, b, group);
         __syncthreads();
         for (int tu = tn; tu > ts; tu -= U) {   // steps tu - 1 down to tu - U
-            T rt[U], rz[U], rg[U];
+            const int n = min(U, tu - ts);
+            float e[U], gy[U];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int t = tu - 1 - i;
-                if (t >= ts && live) {
-                    rt[i] = tp[t * st];
-                    rg[i] = gp[t * sy];
-                    if (zp) rz[i] = zp[t * sz];
+                e[i] = i < n ? step_size(to_f(nt[i]) + dtb, a.softplus) : 0.f;
+                gy[i] = i < n ? to_f(ng[i]) : 0.f;
+                if (gate) {
+                    const float z = to_f(nz[i]);
+                    gy[i] *= z * sigmoidf_(z);
                 }
             }
+            if (n < U) {   // (a stage of fewer steps: only the last one in time; go on from its first row)
+                DT = Walk<T>(a.dt, a.ldt, a.B, b, max(ts - 1, t0), d);
+                DY = Walk<T>(a.dy, a.ldy, a.B, b, max(ts - 1, t0), d);
+                Z = Walk<T>(a.z, a.ldz, a.B, b, max(ts - 1, t0), d);
+            }
+            if (tu - n > t0) fetch(tu - n);
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int t = tu - 1 - i;
-                if (t < ts) break;
-                const float e = step_size(to_f(rt[i]) + dtb, a.softplus);
-                float gy = to_f(rg[i]);
-                if (zp) {
-                    const float z = to_f(rz[i]);
-                    gy *= z * sigmoidf_(z);
-                }
-                const float* row = bc + (t - ts) * 2 * NP + NP;
+                if (i < n) {
+                    const float* row = bc + (tu - 1 - i - ts) * 2 * NP + NP;
 #pragma unroll
-                for (int n = 0; n < NP; ++n) g[n] = fmaf(gy, row[n], g[n]) * exp2_(e * A2[n]);
+                    for (int m = 0; m < NP; ++m) g[m] = fmaf(gy[i], row[m], g[m]) * exp2_(e[i] * A2[m]);
+                }
             }
         }
     }
