@@ -552,7 +552,8 @@ size_t janus_causal_conv_workspace_bytes(const janus_conv_desc* d);
  *           (of s0 where it is shorter); not s0.
  * Errors: NULL d/w, NULL x or y with T > 0, a non-positive D, K, B, T < 0, a
  * stride below D, a pointer not aligned to its element, y = x, or sT = s0 ->
- * INVALID_ARG; K > 8, a dtype or act not listed -> UNSUPPORTED; a length
+ * INVALID_ARG; K > 8, D > 2^24, T > 2^30, a dtype or act not listed ->
+ * UNSUPPORTED; a length
  * outside [0, T] -> LENGTH.
  */
 janus_status janus_causal_conv_fwd(const janus_conv_desc* d, const void* x, const int32_t* lengths,
@@ -632,8 +633,8 @@ size_t janus_selective_scan_workspace_bytes(const janus_scan_desc* d);
  *  y        [T, B, D] dtype; not an input.
  * Errors: NULL d/A, NULL x/dt/Bm/Cm/y with T > 0, a non-positive D, N, G, B,
  * T < 0, D not a multiple of G, a stride below a row, a pointer not aligned to
- * its element -> INVALID_ARG; N > 64, D > 2^22, B times a row stride of x, dt,
- * z or y past 2^29 elements, a dtype or flag not listed -> UNSUPPORTED;
+ * its element -> INVALID_ARG; N > 64, D > 2^22, T > 2^30, B times a row
+ * stride of x, dt, z or y past 2^29 elements, a dtype or flag not listed -> UNSUPPORTED;
  * LENGTH; WORKSPACE.
  */
 janus_status janus_selective_scan_fwd(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
@@ -720,7 +721,7 @@ size_t janus_policy_workspace_bytes(const janus_policy_desc* d);
  * Errors: NULL d/logits/actions, dlogits without old_logp or adv or the
  * reverse, stats when scoring, a non-positive size, ld below V, a bad
  * coefficient, a pointer not aligned to its element -> INVALID_ARG; dtype not
- * F32/BF16 -> UNSUPPORTED; WORKSPACE.
+ * F32/BF16, rows or V past 2^30 -> UNSUPPORTED; WORKSPACE.
  */
 janus_status janus_policy_loss(const janus_policy_desc* d, const void* logits, const int32_t* actions,
                                const float* old_logp, const float* adv, const float* ref_logp,

@@ -16,6 +16,7 @@ namespace janus {
 namespace {
 
 constexpr int kMaxTaps = 8;
+constexpr int kMaxChannels = 1 << 24, kMaxSteps = 1 << 30;   // (32-bit indexes)
 
 struct ConvArgs {
     int32_t D, B, T, seg, nseg;    // seg time steps per segment
@@ -355,7 +356,7 @@ bool conv_desc_ok(const janus_conv_desc* d) {
 janus_status conv_check(const janus_conv_desc* d, const void* x, const void* w, const void* bias, const void* s0,
                         const void* y, const void* sT, bool rows) {
     if (!conv_desc_ok(d) || !w || (rows && (!x || !y))) return JANUS_ERR_INVALID_ARG;
-    if (!dtype_ok(d->dtype) || d->K > kMaxTaps || (d->act != JANUS_CONV_LINEAR && d->act != JANUS_CONV_SILU))
+    if (!dtype_ok(d->dtype) || d->K > kMaxTaps || d->D > kMaxChannels || d->T > kMaxSteps || (d->act != JANUS_CONV_LINEAR && d->act != JANUS_CONV_SILU))
         return JANUS_ERR_UNSUPPORTED;
     const size_t es = dtype_size(d->dtype);
     for (const void* p : {x, w, bias, s0, y, sT})
@@ -480,7 +481,7 @@ size_t conv_ws_bytes(const janus_conv_desc* d) {
 using namespace janus;
 
 extern "C" size_t janus_causal_conv_workspace_bytes(const janus_conv_desc* d) {
-    if (!conv_desc_ok(d) || d->K > kMaxTaps || !dtype_ok(d->dtype)) return 0;
+    if (!conv_desc_ok(d) || d->K > kMaxTaps || d->D > kMaxChannels || !dtype_ok(d->dtype)) return 0;
     return conv_ws_bytes(d);
 }
 
