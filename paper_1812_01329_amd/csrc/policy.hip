@@ -156,15 +156,24 @@ __device__ __forceinline__ S part_of_weights(const PolicyArgs& a) {
     return s;
 }
 
-// The weights that count, added up by one workgroup (the result in thread 0)
-__device__ __forceinline__ double sum_weights(const PolicyArgs& a, double* red) {
-    const double s = wsum(part_of_weights<1024, double>(a));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+// N sums over a workgroup of 1024, in thread 0
+template <int N>
+__device__ __forceinline__ void sum_up(double (&s)[N]) {
+    __shared__ double red[N][16];
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        s[k] = wsum(s[k]);
+        if (lane == 0) red[k][threadIdx.x >> 6] = s[k];
+    }
     __syncthreads();
-    double t = 0.0;
-    if (threadIdx.x == 0)
-        for (int i = 0; i < 16; ++i) t += red[i];
-    return t;
+    if (threadIdx.x >= 64) return;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        s[k] = red[k][lane & 15];
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) s[k] += __shfl_xor(s[k], o, 64);
+    }
 }
 
 // One workgroup a row.  PIECES 16-byte pieces of the row a thread holds; 0: the row is
@@ -342,17 +351,15 @@ __global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
 }
 
 __global__ __launch_bounds__(1024) void policy_weight_kernel(PolicyArgs a) {
-    __shared__ double red[16];
-    const double t = sum_weights(a, red);
-    if (threadIdx.x == 0) *a.W = float(t);
+    double s[1] = {part_of_weights<1024, double>(a)};
+    sum_up(s);
+    if (threadIdx.x == 0) *a.W = float(s[0]);
 }
 
 // the statistics, one workgroup
 __global__ __launch_bounds__(1024) void policy_stats_kernel(PolicyArgs a, float* stats) {
-    __shared__ double red[5][16];
-    const double own = a.own_W ? sum_weights(a, red[4]) : 0.0;
-    double s[4] = {};
-    constexpr int U = 8;
+    double s[5] = {};
+    constexpr int U = 4;
     for (int r0 = threadIdx.x; r0 < a.rows; r0 += U * 1024) {
         float4 t[U];
 #pragma unroll
@@ -361,19 +368,11 @@ __global__ __launch_bounds__(1024) void policy_stats_kernel(PolicyArgs a, float*
         for (int i = 0; i < U; ++i)
             if (r0 + i * 1024 < a.rows) s[0] += t[i].x, s[1] += t[i].y, s[2] += t[i].z, s[3] += t[i].w;
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        s[k] = wsum(s[k]);
-        if ((threadIdx.x & 63) == 0) red[k][threadIdx.x >> 6] = s[k];
-    }
-    __syncthreads();
+    if (a.own_W) s[4] = part_of_weights<1024, double>(a);
+    sum_up(s);
     if (threadIdx.x == 0) {
-        const double W = a.own_W ? own : *a.W;
-        for (int k = 0; k < 4; ++k) {
-            s[k] = 0.0;
-            for (int i = 0; i < 16; ++i) s[k] += red[k][i];
-            s[k] = W > 0.0 ? s[k] / W : 0.0;
-        }
+        const double W = a.own_W ? s[4] : *a.W;
+        for (int k = 0; k < 4; ++k) s[k] = W > 0.0 ? s[k] / W : 0.0;
         stats[0] = float(s[0] + (a.ref ? double(a.beta) * s[1] : 0.0) - (a.eta != 0.f ? double(a.eta) * s[2] : 0.0));
         for (int k = 0; k < 4; ++k) stats[1 + k] = float(s[k]);
         stats[5] = float(W);
