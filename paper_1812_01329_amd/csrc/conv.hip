@@ -10,6 +10,12 @@
 // every row is read once but for K - 1 rows at a segment's edge.  K is a
 // template parameter: a tap padded with a zero weight would turn an infinite
 // input into NaN.
+//
+// Bound by memory.  25600 rows of 1024 bf16 channels, 4 taps, half of the rows
+// past their sequences' ends: forward 18 us (78 MB: 4.3 TB/s), backward 38 us
+// (105 MB: 2.8 TB/s; the rows at segments' edges are read twice, and 164
+// registers a lane leave three waves a SIMD).  One token of 20 rows of 1300:
+// 3.4 us, a launch.
 #include "seq.hpp"
 
 namespace janus {

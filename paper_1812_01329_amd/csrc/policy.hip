@@ -9,8 +9,10 @@
 //
 // One workgroup a row, which it holds in registers from the maximum to the
 // gradient, so the logits are read once and the gradient written once; rows
-// past 64K float32 or 128K bf16 are read three times.  Sums are float32 (float64 over
-// the rows) in a fixed order.
+// past 64K float32 or 128K bf16 are read three times.  Bound by memory: 16384 rows
+// of 32768 bf16 logits 416 us (2.15 GB: 5.2 TB/s; a large copy reaches 4.8);
+// workgroups of 1024 threads, one a CU, took 860.  700 rows of 10000: 12 us, of
+// which 6 are bytes.  Sums are float32 (float64 over the rows) in a fixed order.
 #include <cmath>
 #include <type_traits>
 
