@@ -163,7 +163,8 @@ __global__ __launch_bounds__(256, 2) void scan_fwd_kernel(ScanArgs a, SeqSlice s
         A2[n] = n < a.N ? a.A[d * a.N + n] * kLog2e : 0.f;
         h[n] = 0.f;
     }
-    if (!LOCAL && seg > 0) {
+    // (with segments the first one's start too is the chain's copy: h0 may be hT, which the last segment writes)
+    if (!LOCAL && a.nseg > 1) {
 #pragma unroll
         for (int q = 0; q < NP / 4; ++q) {
             const float4 v = *reinterpret_cast<const float4*>(state_at<NP>(a.seg_h, a, seg, b, q, d));
