@@ -693,6 +693,10 @@ janus_status janus_selective_scan_step(const janus_scan_desc* d, const void* x, 
  * that counts and whose action is V or more, or whose logits hold a NaN or
  * +inf, makes its outputs and the loss NaN (janus_sgd_clip_update then leaves
  * the parameters as they are).  When no row counts, loss and gradient are 0.
+ * With kl_coef 0 a ref changes neither loss nor gradient, only the mean KL
+ * estimate.  That is infinite where u is (a forbidden action, a ref of -inf) or
+ * passes 88, exp(u) of float32; with a kl_coef the loss is then infinite too,
+ * and for u > 0 the row's gradient is infinite or NaN.
  */
 typedef struct {
     int32_t rows, V;

@@ -7,6 +7,7 @@ With l the log-probability of the row's action, r = exp(l - old), u = ref - l:
     row  = -min(r adv, clip(r, 1 - lo, 1 + hi) adv) + beta (exp(u) - 1 - u) - eta H
     loss = sum w row / sum w
 
+The KL term counts only where beta is not 0 (its mean is formed either way).
 Rows of weight 0 or with a negative action do not count (l and H are formed for
 weight 0 all the same); a row of nothing but
 -inf has l = -inf, H = 0 and adds nothing; an action past the vocabulary, a NaN
@@ -61,8 +62,9 @@ def loss(logits, actions, old, adv, ref=None, weights=None, lo=0.2, hi=0.2, beta
         c, kl = (0.0 if off else -free), 0.0
         if ref is not None:
             u = ref[r] - l[r]
-            kl = np.expm1(u) - u
-            c -= beta * np.expm1(u)
+            kl = np.expm1(u) - u if u < np.inf else u
+            if beta:
+                c -= beta * np.expm1(u)
         sums += w[r] * np.array([-(cut if off else free), kl, H[r], float(off)])
         lp = np.where(P[r] > 0.0, np.log(np.where(P[r] > 0.0, P[r], 1.0)), 0.0) if not np.isnan(l[r]) else P[r]
         g = -c * P[r] + eta * P[r] * (lp + H[r])
@@ -70,5 +72,5 @@ def loss(logits, actions, old, adv, ref=None, weights=None, lo=0.2, hi=0.2, beta
             g[actions[r]] += c
         d[r] = g * w[r] / W
     s = sums / W if W > 0.0 else sums
-    total = s[0] + (beta * s[1] if ref is not None else 0.0) - (eta * s[2] if eta else 0.0)
+    total = s[0] + (beta * s[1] if ref is not None and beta else 0.0) - (eta * s[2] if eta else 0.0)
     return dict(stats=np.array([total, *s, W]), logp=l, entropy=H, dlogits=d)

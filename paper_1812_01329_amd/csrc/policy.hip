@@ -61,12 +61,13 @@ __device__ __forceinline__ float rounded_mul(float a, float b) {
     return a * b;
 }
 
-// exp(u) - 1 - u without the cancellation near 0
+// exp(u) - 1 - u without the cancellation near 0 (infinite for an infinite u, also a positive one)
 __device__ __forceinline__ float kl_term(float u) {
     if (fabsf(u) < 0.5f)
         return u * u *
                (0.5f + u * (1.f / 6 + u * (1.f / 24 + u * (1.f / 120 + u * (1.f / 720 + u * (1.f / 5040 + u / 40320))))));
-    return expm1f(u) - u;
+    const float v = expm1f(u);
+    return v == INFINITY ? v : v - u;
 }
 
 template <typename T>
@@ -326,7 +327,7 @@ __global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
     if (a.ref) {
         const float u = ref - l;
         kl = kl_term(u);
-        c -= a.beta * expm1f(u);
+        if (a.beta != 0.f) c -= a.beta * expm1f(u);   // (0 * inf: u of a forbidden action)
     }
     if (tid == 0) a.terms[r] = make_float4(w * -(off ? cut : free_), w * kl, w * H, off ? w : 0.f);
     // gradient p (es (log p + H) - cs), and cs more at the action
@@ -375,7 +376,7 @@ __global__ __launch_bounds__(1024) void policy_stats_kernel(PolicyArgs a, float*
     if (threadIdx.x == 0) {
         const double W = a.own_W ? s[4] : *a.W;
         for (int k = 0; k < 4; ++k) s[k] = W > 0.0 ? s[k] / W : 0.0;
-        stats[0] = float(s[0] + (a.ref ? double(a.beta) * s[1] : 0.0) - (a.eta != 0.f ? double(a.eta) * s[2] : 0.0));
+        stats[0] = float(s[0] + (a.ref && a.beta != 0.f ? double(a.beta) * s[1] : 0.0) - (a.eta != 0.f ? double(a.eta) * s[2] : 0.0));
         for (int k = 0; k < 4; ++k) stats[1 + k] = float(s[k]);
         stats[5] = float(W);
     }
