@@ -26,6 +26,7 @@ constexpr float kFarBelow = -200.f;   // exp is 0 there: keeps 0 * -inf out of t
 
 struct PolicyArgs {
     int32_t rows, V;
+    int32_t row0;         // first row of the launch
     int64_t ld;
     const void* logits;
     const int32_t* actions;
@@ -185,7 +186,7 @@ template <typename T, int PIECES, int THREADS>
 __global__ __launch_bounds__(THREADS, 4) void policy_row_kernel(PolicyArgs a) {
     constexpr int VEC = 16 / sizeof(T), WAVES = THREADS / 64;
     __shared__ float red[4][WAVES];
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r = a.row0 + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool score = !a.dlogits;
     const int act = a.actions[r];
     const float w = !score && a.weights ? a.weights[r] : 1.f;
@@ -397,9 +398,13 @@ size_t policy_carve(PolicyArgs& a, int rows, void* ws) {
 // Up to this many rows each workgroup adds the weights up itself: a launch less.
 constexpr int kOwnWeightRows = 2048;
 
+// A launch holds fewer than 2^32 threads: more rows take several.
 template <typename T, int PIECES, int THREADS>
-void row_launch(const PolicyArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((policy_row_kernel<T, PIECES, THREADS>), dim3(a.rows), dim3(THREADS), 0, st, a);
+void row_launch(PolicyArgs a, hipStream_t st) {
+    constexpr int kMost = (1 << 30) / THREADS * 2;
+    for (; a.row0 < a.rows; a.row0 += kMost)
+        hipLaunchKernelGGL((policy_row_kernel<T, PIECES, THREADS>), dim3(std::min(kMost, a.rows - a.row0)),
+                           dim3(THREADS), 0, st, a);
 }
 // The fewest pieces a thread that hold a row (which may touch one piece more
 // than its length fills), since every pass works on all of them: small
