@@ -688,44 +688,49 @@ __global__ __launch_bounds__(64 * kBwdWaves, NP <= 16 ? 4 : NP == 32 ? 2 : 1) vo
     }
 }
 
-// dA, dDskip, ddt_bias: 64 values a workgroup, each wave sums every 16th part,
-// then the waves' sums in their order.
+// dA, dDskip, ddt_bias: 64 values at a time a workgroup, each wave sums every
+// 16th part, then the waves' sums in their order.
 __global__ __launch_bounds__(1024) void scan_param_kernel(const float* dA_part, const float* dv_part, int parts, int D,
                                                           int N, float* dA, float* dD, float* ddtb) {
     __shared__ float red[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i = int64_t(blockIdx.x) * 64 + lane, na = int64_t(D) * N;
-    const bool on = i < na + 2 * D;
-    const float* p = i < na ? dA_part + i : dv_part + (i - na);
-    const int64_t step = i < na ? na : 2 * int64_t(D);
-    float v = 0.f;
-    if (on)
-        for (int k = wave; k < parts; k += 16) v += p[k * step];
-    red[wave][lane] = v;
-    __syncthreads();
-    if (wave != 0 || !on) return;
-    for (int w = 1; w < 16; ++w) v += red[w][lane];
-    if (i < na) dA[i] = v;
-    else if (i < na + D) {
-        if (dD) dD[i - na] = v;
-    } else if (ddtb) {
-        ddtb[i - na - D] = v;
+    const int64_t na = int64_t(D) * N, all = na + 2 * int64_t(D);
+    for (int64_t i0 = int64_t(blockIdx.x) * 64; i0 < all; i0 += int64_t(gridDim.x) * 64) {
+        const int64_t i = i0 + lane;
+        const bool on = i < all;
+        const float* p = i < na ? dA_part + i : dv_part + (i - na);
+        const int64_t step = i < na ? na : 2 * int64_t(D);
+        float v = 0.f;
+        if (on)
+            for (int k = wave; k < parts; k += 16) v += p[k * step];
+        red[wave][lane] = v;
+        __syncthreads();
+        if (wave == 0 && on) {
+            for (int w = 1; w < 16; ++w) v += red[w][lane];
+            if (i < na) dA[i] = v;
+            else if (i < na + D) {
+                if (dD) dD[i - na] = v;
+            } else if (ddtb) {
+                ddtb[i - na - D] = v;
+            }
+        }
+        __syncthreads();
     }
 }
 
 // dB and dC: the workgroups' parts of each row
 template <typename T, int NP>
 __global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a) {
-    const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, rows = int64_t(a.T) * a.B;
-    const int64_t all = rows * a.G * 2 * NP;
-    if (i >= all) return;
-    const int m = int(i % (2 * NP)), n = m % NP, group = int(i / (2 * NP) % a.G);
-    const int64_t row = i / (2 * NP) / a.G;
-    if (n >= a.N) return;
-    float v = 0.f;
-    for (int k = 0; k < a.bblocks; ++k) v += a.bc_part[k * all + i];
-    if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = out_f<T>(v);
-    else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = out_f<T>(v);
+    const int64_t rows = int64_t(a.T) * a.B, all = rows * a.G * 2 * NP;
+    for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += int64_t(gridDim.x) * blockDim.x) {
+        const int m = int(i % (2 * NP)), n = m % NP, group = int(i / (2 * NP) % a.G);
+        const int64_t row = i / (2 * NP) / a.G;
+        if (n >= a.N) continue;
+        float v = 0.f;
+        for (int k = 0; k < a.bblocks; ++k) v += a.bc_part[k * all + i];
+        if (m < NP) static_cast<T*>(a.dBm)[row * a.ldb + int64_t(group) * a.N + n] = out_f<T>(v);
+        else static_cast<T*>(a.dCm)[row * a.ldc + int64_t(group) * a.N + n] = out_f<T>(v);
+    }
 }
 
 // One token: QL lanes per channel with 4 states each.  Bound by the states' bytes:
@@ -880,6 +885,9 @@ void scan_inputs(ScanArgs& a, const void* x, const void* dt, const float* A, con
     a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.Dskip = Dskip, a.z = z, a.dtb = dt_bias;
 }
 
+// A launch holds fewer than 2^32 threads; kernels of more loop.
+dim3 launch_blocks(int64_t blocks, int threads) { return dim3(std::min<int64_t>(blocks, (int64_t(1) << 31) / threads)); }
+
 dim3 scan_block(const ScanArgs& a) { return dim3(64 * std::min(kScanWaves, a.tiles)); }
 
 template <typename T, int NP>
@@ -939,14 +947,14 @@ janus_status scan_bwd_run(const ScanArgs& a, const int32_t* lengths, float* dA, 
     {
         const int parts = a.nseg * a.B;
         TraceScope trace("scan_param", double(np) * parts, 4.0 * np * parts, st);
-        hipLaunchKernelGGL(scan_param_kernel, dim3((np + 63) / 64), dim3(1024), 0, st, a.dA_part, a.dv_part, parts, a.D,
-                           a.N, dA, dDskip, ddt_bias);
+        hipLaunchKernelGGL(scan_param_kernel, launch_blocks((np + 63) / 64, 1024), dim3(1024), 0, st, a.dA_part,
+                           a.dv_part, parts, a.D, a.N, dA, dDskip, ddt_bias);
         JANUS_LAUNCH_CHECK();
     }
     if (a.bc_part && a.T > 0) {
         const int64_t all = int64_t(a.T) * a.B * a.G * 2 * NP;
         TraceScope trace("scan_bc", double(all) * a.bblocks, 4.0 * all * a.bblocks, st);
-        hipLaunchKernelGGL((scan_bc_kernel<T, NP>), dim3((all + 255) / 256), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((scan_bc_kernel<T, NP>), launch_blocks((all + 255) / 256, 256), dim3(256), 0, st, a);
         JANUS_LAUNCH_CHECK();
     }
     return JANUS_OK;
