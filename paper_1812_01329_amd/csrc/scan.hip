@@ -818,7 +818,7 @@ bool scan_desc_ok(const janus_scan_desc* d) {
 bool scan_supported(const janus_scan_desc* d) {
     return dtype_ok(d->dtype) && d->N <= kMaxStates && (d->flags & ~(JANUS_SCAN_SOFTPLUS | JANUS_SCAN_KEEP)) == 0 &&
            d->T <= (1 << 30) && d->D <= (1 << 22) && d->B <= (1 << 24) &&
-           d->B * std::max({d->ldx, d->ldt, d->ldz, d->ldy, int64_t(d->D)}) <= (int64_t(1) << 29);
+           std::max({d->ldx, d->ldt, d->ldz, d->ldy, int64_t(d->D)}) <= (int64_t(1) << 29) / d->B;
 }
 // states rounded up to what the kernels are built for
 int padded_states(int N) { return N <= 4 ? 4 : N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
