@@ -567,9 +567,10 @@ janus_status janus_causal_conv_fwd(const janus_conv_desc* d, const void* x, cons
  *  dx       [T, B, D] dtype, row stride ldx, or NULL; 0 from lengths[b] on;
  *           not x or dy.
  *  dw [D, K], dbias [D]: float32, either may be NULL.
- *  ds0      [B, K-1, D] float32 or NULL.
+ *  ds0      [B, K-1, D] float32 or NULL; not dsT.
  * The sums over time and batch are taken in a fixed order.
- * Errors: as the forward; NULL dy with T > 0 -> INVALID_ARG; WORKSPACE.
+ * Errors: as the forward; NULL dy with T > 0, dx = x or dy, ds0 = dsT ->
+ * INVALID_ARG; WORKSPACE.
  */
 janus_status janus_causal_conv_bwd(const janus_conv_desc* d, const void* x, const int32_t* lengths,
                                    const void* w, const void* bias, const void* s0, const void* dy,

@@ -521,8 +521,10 @@ extern "C" janus_status janus_causal_conv_bwd(const janus_conv_desc* d, const vo
                                               void* ws, size_t ws_bytes, void* stream) {
     janus_status e = conv_check(d, x, w, bias, s0, dy, dx, d && d->T > 0);
     if (e != JANUS_OK) return e;
-    if ((dx && (dx == x || dx == dy)) || !aligned(dsT, 4) || !aligned(dw, 4) || !aligned(dbias, 4) || !aligned(ds0, 4))
-        return JANUS_ERR_INVALID_ARG;
+    if ((dx && (dx == x || dx == dy)) || (ds0 && ds0 == dsT)) return JANUS_ERR_INVALID_ARG;
+    for (const float* p : {dsT, static_cast<const float*>(dw), static_cast<const float*>(dbias),
+                           static_cast<const float*>(ds0)})
+        if (!aligned(p, 4)) return JANUS_ERR_INVALID_ARG;
     if ((e = check_lengths(d->B, d->T, lengths)) != JANUS_OK) return e;
     if (!ws || ws_bytes < conv_ws_bytes(d) || !aligned(ws, 256)) return JANUS_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
