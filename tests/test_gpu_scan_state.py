@@ -79,7 +79,8 @@ def test_training_over_segments(T, B, D, N, G, lengths, dtype):
 
 
 @pytest.mark.parametrize("dtype,T,D,N,G", [("f32", 150, 40, 16, 1), ("bf16", 150, 66, 13, 2), ("f32", 20, 70, 64, 1),
-                                           ("bf16", 20, 64, 16, 1)])
+                                           ("bf16", 20, 64, 16, 1), ("f32", 20, 33, 12, 1), ("bf16", 20, 36, 20, 3),
+                                           ("bf16", 20, 40, 36, 1)])
 def test_a_prompt_continued_by_single_tokens(dtype, T, D, N, G):
     """The final states of ragged prompts (with the time axis cut and not), put
     into slots of a larger state and moved on token by token, give what the
