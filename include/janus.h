@@ -553,8 +553,7 @@ size_t janus_causal_conv_workspace_bytes(const janus_conv_desc* d);
  * Errors: NULL d/w, NULL x or y with T > 0, a non-positive D, K, B, T < 0, a
  * stride below D, a pointer not aligned to its element, y = x, or sT = s0 ->
  * INVALID_ARG; K > 8, D > 2^24, T > 2^30, a dtype or act not listed ->
- * UNSUPPORTED; a length
- * outside [0, T] -> LENGTH.
+ * UNSUPPORTED; a length outside [0, T] -> LENGTH.
  */
 janus_status janus_causal_conv_fwd(const janus_conv_desc* d, const void* x, const int32_t* lengths,
                                    const void* w, const void* bias, const void* s0, void* y, void* sT,
@@ -586,7 +585,8 @@ janus_status janus_causal_conv_bwd(const janus_conv_desc* d, const void* x, cons
  *           rows have slots of their own.
  *  state    [n_slots, K-1, D] dtype, updated in place (sT of a prompt is
  *           such a state).  May be NULL when K is 1.
- * Errors: as the forward; n_slots < 1 (or < B with slots NULL) -> INVALID_ARG.
+ * Errors: as the forward; n_slots < 1 (or < B with slots NULL) -> INVALID_ARG;
+ * B > 65535 -> UNSUPPORTED.
  */
 janus_status janus_causal_conv_step(const janus_conv_desc* d, const void* x, const void* w, const void* bias,
                                     const int32_t* slots, int32_t n_slots, void* state, void* y, void* stream);
@@ -603,7 +603,8 @@ janus_status janus_causal_conv_step(const janus_conv_desc* d, const void* x, con
  *     y_t[d] = (sum_n C_t[g, n] h_t[d, n] + Dskip[d] x_t[d]) * (z_t[d] s(z_t[d]))
  * with g = d / (D / G), the last factor only with a gate z.  Sequence b runs
  * while t < lengths[b]; its state is then carried unchanged and its y is 0
- * (nothing of its later rows is read).
+ * (nothing of its later rows is read).  Where an input makes a state infinite or
+ * NaN, what depends on that state is infinite or NaN, and which is not defined.
  */
 #define JANUS_SCAN_SOFTPLUS 1   /* e = log(1 + exp(v)) */
 #define JANUS_SCAN_KEEP 2       /* the forward keeps in the workspace what its backward needs */
@@ -630,13 +631,14 @@ size_t janus_selective_scan_workspace_bytes(const janus_scan_desc* d);
  *  A        [D, N] float32 (the exponent e A is a product that spans orders
  *           of magnitude; 16 bits would move the slow decays);  Dskip,
  *           dt_bias [D] float32 or NULL (zero).
- *  h0, hT   [B, D, N] float32 or NULL (zeros; not wanted); hT may be h0.
+ *  h0, hT   [B, D, N] float32 or NULL (zeros; not wanted); hT may be h0, but
+ *           with KEEP, whose backward reads h0.
  *  y        [T, B, D] dtype; not an input.
  * Errors: NULL d/A, NULL x/dt/Bm/Cm/y with T > 0, a non-positive D, N, G, B,
  * T < 0, D not a multiple of G, a stride below a row, a pointer not aligned to
- * its element -> INVALID_ARG; N > 64, D > 2^22, T > 2^30, B times a row
- * stride of x, dt, z or y past 2^29 elements, a dtype or flag not listed -> UNSUPPORTED;
- * LENGTH; WORKSPACE.
+ * its element, y an input, hT = h0 with KEEP -> INVALID_ARG; N > 64, D > 2^22,
+ * T > 2^30, B > 2^24, B times a row stride of x, dt, z or y past 2^29 elements, a
+ * dtype or flag not listed -> UNSUPPORTED; LENGTH; WORKSPACE.
  */
 janus_status janus_selective_scan_fwd(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
                                       const void* Bm, const void* Cm, const float* Dskip, const void* z,
@@ -653,7 +655,8 @@ janus_status janus_selective_scan_fwd(const janus_scan_desc* d, const void* x, c
  *  dA [D, N], dDskip, ddt_bias [D], dh0 [B, D, N]: float32; the last three
  *           may be NULL.  The sums are taken in a fixed order.
  * Errors: as the forward; NULL dy/dx/ddt/dBm/dCm with T > 0, NULL dA, NULL dz
- * with z, or a descriptor without KEEP -> INVALID_ARG.
+ * with z, a row gradient in the place of an input or dy, or a descriptor without
+ * KEEP -> INVALID_ARG.
  */
 janus_status janus_selective_scan_bwd(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
                                       const void* Bm, const void* Cm, const float* Dskip, const void* z,
@@ -668,7 +671,8 @@ janus_status janus_selective_scan_bwd(const janus_scan_desc* d, const void* x, c
  *  slots, n_slots  as janus_causal_conv_step.
  *  state    [n_slots, D, N] float32, updated in place (hT of a prompt is such
  *           a state).
- * Errors: as the forward; n_slots < 1 (or < B with slots NULL) -> INVALID_ARG.
+ * Errors: as the forward; n_slots < 1 (or < B with slots NULL) -> INVALID_ARG;
+ * B > 65535 -> UNSUPPORTED.
  */
 janus_status janus_selective_scan_step(const janus_scan_desc* d, const void* x, const void* dt, const float* A,
                                        const void* Bm, const void* Cm, const float* Dskip, const void* z,

@@ -13,9 +13,12 @@
 //
 // Bound by memory.  25600 rows of 1024 bf16 channels, 4 taps, half of the rows
 // past their sequences' ends: forward 18 us (78 MB: 4.3 TB/s), backward 38 us
-// (105 MB: 2.8 TB/s; the rows at segments' edges are read twice, and 164
-// registers a lane leave three waves a SIMD).  One token of 20 rows of 1300:
-// 3.4 us, a launch.
+// (105 MB: 2.8 TB/s; the rows at segments' edges are read twice, and two waves
+// stand on a SIMD: 163 registers a lane would leave room for a third, but not
+// for a second workgroup of eight waves on a CU).  All rows within the sequences:
+// bf16 21 and 51 us, float32 34 and 69 us, float32 with 8 taps 37 and 195 us (7
+// and 8 taps of four float32 channels spill 16 and 83 registers in the backward).
+// One token of 20 rows of 1300: 3.4 us, a launch.
 #include "seq.hpp"
 
 namespace janus {

@@ -25,9 +25,13 @@
 // number of waves shares a SIMD (5.4 with one wave, 3.6 with three), 4.3 with a
 // scalar or constant operand or a lane exchange, 8.3 for an exponential or a
 // reciprocal.  So B and C come from LDS in vector registers and not from
-// scalar ones, and the kernels are held to 128 registers: four waves.
+// scalar ones.  Up to 16 states four waves stand on a SIMD: the forward takes 121
+// registers, the backward is held to 128 (with 16 states it spills 12 of them with
+// a gate and 3 without).  Past 16 states there is room for two in the backward,
+// past 32 for one.
 // 65536 rows of 2048 bf16 channels, 16 states: forward 0.59 ms (0.27 of these
-// operations alone), backward 1.83 ms (0.72), 1.1 and 1.5 TB/s.
+// operations alone), backward 1.83 ms (0.72), 1.1 and 1.5 TB/s.  25600 rows of
+// 1024 channels: 0.14 and 0.39 ms with 16 states, 0.55 and 2.1 with 64.
 #include <type_traits>
 
 #include "seq.hpp"
