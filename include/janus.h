@@ -628,7 +628,7 @@ size_t janus_selective_scan_workspace_bytes(const janus_scan_desc* d);
  *  x, dt    [T, B, D] dtype;  Bm, Cm [T, B, G, N] dtype;  z [T, B, D] dtype
  *           or NULL (no gate).
  *  lengths  host int32 [B] with 0 <= len <= T, or NULL for all T.
- *  A        [D, N] float32 (the exponent e A is a product that spans orders
+ *  A        [D, N] float32, finite (the exponent e A is a product that spans orders
  *           of magnitude; 16 bits would move the slow decays);  Dskip,
  *           dt_bias [D] float32 or NULL (zero).
  *  h0, hT   [B, D, N] float32 or NULL (zeros; not wanted); hT may be h0, but

@@ -26,9 +26,8 @@
 // scalar or constant operand or a lane exchange, 8.3 for an exponential or a
 // reciprocal.  So B and C come from LDS in vector registers and not from
 // scalar ones.  Up to 16 states four waves stand on a SIMD: the forward takes 121
-// registers, the backward is held to 128 (with 16 states it spills 12 of them with
-// a gate and 3 without).  Past 16 states there is room for two in the backward,
-// past 32 for one.
+// registers, the backward is held to 128 (with 16 states and a gate it spills 8 of
+// them).  Past 16 states there is room for two in the backward, past 32 for one.
 // 65536 rows of 2048 bf16 channels, 16 states: forward 0.59 ms (0.27 of these
 // operations alone), backward 1.83 ms (0.72), 1.1 and 1.5 TB/s.  25600 rows of
 // 1024 channels: 0.14 and 0.39 ms with 16 states, 0.55 and 2.1 with 64.
@@ -594,6 +593,12 @@ __global__ __launch_bounds__(64 * kBwdWaves, NP <= 16 ? 4 : NP == 32 ? 2 : 1) vo
 #pragma unroll
             for (int k = k0 + HK - 1; k >= k0; --k) {
                 __builtin_amdgcn_sched_barrier(0);
+                // Past the end G stays; the sums would be 0 times what may be infinite.  (Said to be unlikely: otherwise
+                // the compiler's order of the code costs the backward 2 %.)
+                if (__builtin_expect(tc + k >= lim, 0)) {
+                    odd[0] = odd[1] = odd[2] = 0.f;
+                    continue;
+                }
                 const float2 e2 = *reinterpret_cast<const float2*>(&sh[wave][0][k][2 * c16]);
                 const float2 u2 = *reinterpret_cast<const float2*>(&sh[wave][1][k][2 * c16]);
                 const float2 g2 = *reinterpret_cast<const float2*>(&sh[wave][2][k][2 * c16]);
@@ -642,7 +647,7 @@ __global__ __launch_bounds__(64 * kBwdWaves, NP <= 16 ? 4 : NP == 32 ? 2 : 1) vo
                     dtbs += ddt;
                     float dz = 0.f;
                     if (GATE) dz = sh[wave][GATE ? 5 : 0][k + half][own] * fmaf(dskip, x, fold32(fy, odd[2]));
-                    if (k + half < tn && live) {   // 0 past the sequence's end: e, u, gy, x are
+                    if (tc + k + half < lim && live) {
                         *rx.at(DX, tc + k) = out_f<T>(fmaf(ogy, dskip, oe * S));
                         *rt.at(DDT, tc + k) = out_f<T>(ddt);
                         if (GATE) *rz.at(DZ, tc + k) = out_f<T>(dz);
@@ -650,9 +655,11 @@ __global__ __launch_bounds__(64 * kBwdWaves, NP <= 16 ? 4 : NP == 32 ? 2 : 1) vo
                 }
             }
             }
-        } else if (live) {
-            for (int k = 0; k < tn; k += 2) {
-                if (k + half >= tn) continue;
+        }
+        const bool ends = lim < tc + tn;
+        if (__builtin_expect(ends, 0) && live) {   // 0 in the rows past the sequence's end
+            for (int k = max(lim - tc, 0) & ~1; k < tn; k += 2) {
+                if (tc + k + half < lim || k + half >= tn) continue;
                 *rx.at(DX, tc + k) = out_f<T>(0.f);
                 *rt.at(DDT, tc + k) = out_f<T>(0.f);
                 if (GATE) *rz.at(DZ, tc + k) = out_f<T>(0.f);
