@@ -738,6 +738,122 @@ janus_status janus_policy_loss(const janus_policy_desc* d, const void* logits, c
                                void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Layer norm                                                               */
+/* ------------------------------------------------------------------------ */
+/*
+ * Rows brought to mean 0 and variance 1, scaled and shifted, after the residual
+ * sum that goes before it in a stack of layers:
+ *     h = x + r (rounded to dtype; h = x without r)
+ *     mean = sum h / D,  rstd = 1 / sqrt(sum (h - mean)^2 / D + eps)
+ *     y = (h - mean) rstd gamma + beta
+ * Rows are independent: a row with an infinity or a NaN has NaN in its y and
+ * dx, and in dgamma and dbeta.  Every row counts for those two; rows past a
+ * sequence's end add nothing where their dy is 0 and their h finite.
+ */
+/* The ld* are the row strides, in elements, of x and dx (ldx), of r, h and dh
+ * (ldh) and of y and dy (ldy); 0: dense, D; else at least D. */
+typedef struct {
+    int32_t rows, D;
+    janus_dtype dtype;
+    float eps;              /* finite, not negative */
+    int64_t ldx, ldh, ldy;
+} janus_norm_desc;
+
+/* Bytes of workspace of janus_layer_norm_bwd (0 for a bad descriptor or no rows). */
+size_t janus_layer_norm_workspace_bytes(const janus_norm_desc* d);
+
+/*
+ *  x        [rows, D] dtype;  r [rows, D] dtype or NULL (no residual).
+ *  gamma, beta [D] float32, each may be NULL (ones; zeros).
+ *  h        [rows, D] dtype or NULL: the sum x + r as the backward reads it; may
+ *           be r or x (with its stride).  Only with r.
+ *  y        [rows, D] dtype; not x, r or h.
+ *  mean, rstd [rows] float32, each may be NULL (not wanted: no backward).
+ * Errors: NULL d, NULL x or y with rows > 0, h without r, D < 1, rows < 0, a
+ * stride below D, an eps that is negative or not finite, a pointer not aligned to
+ * its element, y = x, r or h, h = x with another stride -> INVALID_ARG; dtype not
+ * F32/BF16, rows past 2^30 or D past 2^24 -> UNSUPPORTED.
+ */
+janus_status janus_layer_norm_fwd(const janus_norm_desc* d, const void* x, const void* r,
+                                  const float* gamma, const float* beta, void* h, void* y,
+                                  float* mean, float* rstd, void* stream);
+
+/*
+ * Backward of the call above.  With xh = (h - mean) rstd and g = dy gamma:
+ *     dx = rstd (g - sum g / D - xh sum(g xh) / D) + dh
+ *     dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
+ * dx is the gradient of x and of r.
+ *  h        [rows, D] dtype, row stride ldh: the forward's h, or its x where it
+ *           had no residual (ldh is then x's stride).
+ *  mean, rstd [rows] float32 of the forward.
+ *  dy       [rows, D] dtype, row stride ldy.
+ *  dh       [rows, D] dtype, row stride ldh, or NULL (zero): the gradient that h
+ *           has from where else it goes.
+ *  dx       [rows, D] dtype, row stride ldx, or NULL; may be dh (with its
+ *           stride); not h or dy.
+ *  dgamma, dbeta [D] float32, each may be NULL.  The sums are taken in a fixed order.
+ * Errors: as the forward; NULL h, mean, rstd or dy with rows > 0, dx = h or dy, dx =
+ * dh with another stride -> INVALID_ARG; WORKSPACE (not looked at when dgamma and
+ * dbeta are both NULL, or without rows).
+ */
+janus_status janus_layer_norm_bwd(const janus_norm_desc* d, const void* h, const float* gamma,
+                                  const float* mean, const float* rstd, const void* dy, const void* dh,
+                                  void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                                  void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Drawing tokens                                                           */
+/* ------------------------------------------------------------------------ */
+/*
+ * One token from each row of logits by a given uniform number.  With the
+ * weights w = exp((x - max x) / T) and tokens ordered by falling x, equal ones
+ * by rising index, the tokens kept are those that are
+ *     among the first top_k,
+ *     in the shortest run from the front with at least top_p of the weight of
+ *     those (the first one always is), and
+ *     of a weight of at least min_p (largest: 1).
+ * The token is the first one, by index, up to which the weights of the kept ones
+ * pass u times their sum.  A top_k <= 0, a top_p >= 1 and a min_p <= 0 keep all;
+ * a min_p above 1 counts as 1; T = 0 keeps the first of the largest logits only.
+ * A u below 0 counts as 0, one from 1 on draws the last token of weight.  Weights and sums are
+ * taken in 64 bits, so a token does not depend on the order of a sum.
+ * Logits of -inf (forbidden tokens) are never kept.  A row with nothing but
+ * -inf has token -1, kept 0 and log-probabilities -inf; one with a NaN or +inf
+ * logit, a NaN setting or u, or a negative T has token -1, kept 0 and
+ * log-probabilities NaN.
+ */
+typedef struct {
+    int32_t rows, V;
+    janus_dtype dtype;
+    int64_t ld;             /* elements between rows of logits; 0: V */
+    float temperature;      /* not negative, not NaN */
+    int32_t top_k;
+    float top_p, min_p;     /* not NaN */
+} janus_sample_desc;
+
+/* Bytes of workspace of janus_sample (0 for a bad descriptor; may be 0). */
+size_t janus_sample_workspace_bytes(const janus_sample_desc* d);
+
+/*
+ *  logits   [rows, V] dtype, row stride ld.
+ *  u        [rows] float32, uniform in [0, 1).
+ *  temperature, top_p, min_p [rows] float32, top_k [rows] int32: device, each may be
+ *           NULL (d's for every row); checked on the device (above).
+ *  tokens   device int32 [rows].
+ *  logp     [rows] float32 or NULL: the token's log-probability in softmax(x), as
+ *           janus_policy_loss has it (T = 1, nothing filtered).
+ *  draw_logp [rows] float32 or NULL: its log-probability among the kept.
+ *  kept     int32 [rows] or NULL: how many tokens were kept.
+ * Errors: NULL d/logits/u/tokens, a non-positive size, ld below V, a temperature
+ * that is negative, or a NaN in d, a pointer not aligned to its element -> INVALID_ARG;
+ * dtype not F32/BF16, V past 2^24, rows past 2^30 -> UNSUPPORTED; WORKSPACE.
+ */
+janus_status janus_sample(const janus_sample_desc* d, const void* logits, const float* u,
+                          const float* temperature, const int32_t* top_k, const float* top_p,
+                          const float* min_p, int32_t* tokens, float* logp, float* draw_logp,
+                          int32_t* kept, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Tracing                                                                  */
 /* ------------------------------------------------------------------------ */
 
@@ -839,6 +955,73 @@ janus_status janus_sgd_clip_update(const janus_sgd_desc* d, void* const* params,
 janus_status janus_sgd_clip_update_noalloc(const janus_sgd_desc* d, void* const* params,
                                            const float* const* grads, const int64_t* sizes,
                                            float* stats, const uint32_t* hold, void* stream);
+
+/*
+ * AdamW on many tensors in one call: the SGD update's rule for the gradients'
+ * global norm, then moments of the scaled gradients and a step by them, with a
+ * decay of the weights apart from the gradient.  With t the number of the step
+ * (from 1) and s as in janus_sgd_clip_update:
+ *     g <- s g,   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
+ *     p <- p - lr decay p - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in float32; with a master copy p is that, and the parameter its rounding.
+ * All-or-nothing as there: a norm that is not finite, or `hold`, leaves every
+ * parameter, state and the count of steps as they are.
+ *
+ * ADAMW_F32 states are m and v, float32 [size] each, zero at first.
+ * ADAMW_8BIT states are m and sqrt(v) as 8-bit floats (e4m3: sign, 4 exponent and
+ * 3 mantissa bits, largest 448), uint8 [size] each, times a power of two for each
+ * of the two and every 256 elements, float32 [ceil(size / 256)][2] (m's, then
+ * sqrt(v)'s, 8-byte aligned); both zero at first.  The power is the least that keeps the largest
+ * of the 256 within 448 (and not below 2^-126).  They are rounded up or down with
+ * the probability that keeps their mean (a step moves v by 0.1 %, which rounding
+ * to the nearest of codes 12 % apart would lose), by bits that seed, step, the
+ * tensor's place and the element's index decide, so repeated calls give the same result.
+ */
+typedef enum { JANUS_ADAMW_F32 = 0, JANUS_ADAMW_8BIT = 1 } janus_adamw_states;
+
+typedef struct {
+    int32_t n;              /* tensors, >= 1 */
+    janus_adamw_states states;
+    float lr;               /* finite */
+    float beta1, beta2;     /* in [0, 1) */
+    float eps;              /* finite, > 0 */
+    float max_norm;         /* as in janus_sgd_desc */
+    uint32_t seed;          /* of the 8-bit states' rounding */
+} janus_adamw_desc;
+
+/* One tensor, flat and contiguous: device pointers, which may be NULL where size is 0. */
+typedef struct {
+    void* p;                /* parameters, updated in place */
+    const float* g;         /* float32 gradients */
+    void *m, *v;            /* states, updated in place */
+    float* scale;           /* of 8-bit states, updated in place; else not looked at */
+    float* master;          /* float32 copy of bf16 parameters, updated in place, or NULL */
+    int64_t size;
+    float decay;            /* finite */
+    janus_dtype dtype;      /* of p */
+} janus_adamw_tensor;
+
+/* Workspace bytes for janus_adamw_update with this descriptor (0 for a bad
+ * descriptor). */
+size_t janus_adamw_workspace_bytes(const janus_adamw_desc* d);
+
+/*
+ *  tensors  host array of n; they must not overlap.
+ *  step     device int64: steps taken so far (0 at first), raised by one when
+ *           the update is applied, so that a captured call goes on counting.
+ *  lr       device float32 or NULL (d->lr): read when the update runs, so that a
+ *           captured call can follow a schedule.  One that is not finite holds
+ *           the update.
+ *  stats, hold  as in janus_sgd_clip_update.
+ * Errors: NULL d/tensors/step, n < 1, a number of d or a decay outside its range, a
+ * negative size, a NULL pointer of a non-empty tensor (scale with 8-bit states), a
+ * master of float32 parameters, a pointer not aligned to its element -> INVALID_ARG;
+ * states or dtype not listed, a tensor past 2^40 elements (2^32 with 8-bit states) ->
+ * UNSUPPORTED; WORKSPACE.
+ */
+janus_status janus_adamw_update(const janus_adamw_desc* d, const janus_adamw_tensor* tensors,
+                                int64_t* step, const float* lr, float* stats, const uint32_t* hold,
+                                void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Misc                                                                     */

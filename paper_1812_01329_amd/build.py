@@ -20,7 +20,7 @@ OUT = os.path.join(PKG, "libjanus.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
 SOURCES = ["schedule.cpp", "runtime.cpp", "gemm.hip", "lstm.hip", "heads.hip", "tree.hip", "sgd.hip", "childsum.hip",
-           "conv.hip", "scan.hip", "policy.hip"]
+           "conv.hip", "scan.hip", "policy.hip", "norm.hip", "adamw.hip", "sample.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

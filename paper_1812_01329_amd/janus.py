@@ -25,6 +25,7 @@ EMBED_FWD, XENT_FWD_BWD, EMBED_BWD = 0, 1, 2
 LOSS_SUMSQ, LOSS_MEAN = 0, 1
 CONV_LINEAR, CONV_SILU = 0, 1
 SCAN_SOFTPLUS, SCAN_KEEP = 1, 2
+ADAMW_F32, ADAMW_8BIT = 0, 1
 
 EXPORTS = [
     "janus_lstm_workspace_bytes", "janus_lstm_seq_fwd", "janus_lstm_seq_bwd", "janus_lstm_device_report",
@@ -40,6 +41,8 @@ EXPORTS = [
     "janus_causal_conv_workspace_bytes", "janus_causal_conv_fwd", "janus_causal_conv_bwd", "janus_causal_conv_step",
     "janus_selective_scan_workspace_bytes", "janus_selective_scan_fwd", "janus_selective_scan_bwd",
     "janus_selective_scan_step", "janus_policy_workspace_bytes", "janus_policy_loss",
+    "janus_layer_norm_workspace_bytes", "janus_layer_norm_fwd", "janus_layer_norm_bwd",
+    "janus_sample_workspace_bytes", "janus_sample", "janus_adamw_workspace_bytes", "janus_adamw_update",
 ]
 
 
@@ -107,6 +110,26 @@ class ScanDesc(C.Structure):
 class PolicyDesc(C.Structure):
     _fields_ = [("rows", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int), ("ld", C.c_int64),
                 ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float), ("ent_coef", C.c_float)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int), ("eps", C.c_float), ("ldx", C.c_int64),
+                ("ldh", C.c_int64), ("ldy", C.c_int64)]
+
+
+class SampleDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int), ("ld", C.c_int64),
+                ("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
+
+
+class AdamWDesc(C.Structure):
+    _fields_ = [("n", C.c_int32), ("states", C.c_int), ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float),
+                ("eps", C.c_float), ("max_norm", C.c_float), ("seed", C.c_uint32)]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("scale", C.c_void_p),
+                ("master", C.c_void_p), ("size", C.c_int64), ("decay", C.c_float), ("dtype", C.c_int)]
 
 
 _lib = None
@@ -188,6 +211,16 @@ def lib():
         L.janus_policy_workspace_bytes.restype = sz
         L.janus_policy_workspace_bytes.argtypes = [C.POINTER(PolicyDesc)]
         L.janus_policy_loss.argtypes = [C.POINTER(PolicyDesc)] + [vp] * 11 + [sz, vp]
+        L.janus_layer_norm_workspace_bytes.restype = sz
+        L.janus_layer_norm_workspace_bytes.argtypes = [C.POINTER(NormDesc)]
+        L.janus_layer_norm_fwd.argtypes = [C.POINTER(NormDesc)] + [vp] * 9
+        L.janus_layer_norm_bwd.argtypes = [C.POINTER(NormDesc)] + [vp] * 10 + [sz, vp]
+        L.janus_sample_workspace_bytes.restype = sz
+        L.janus_sample_workspace_bytes.argtypes = [C.POINTER(SampleDesc)]
+        L.janus_sample.argtypes = [C.POINTER(SampleDesc)] + [vp] * 11 + [sz, vp]
+        L.janus_adamw_workspace_bytes.restype = sz
+        L.janus_adamw_workspace_bytes.argtypes = [C.POINTER(AdamWDesc)]
+        L.janus_adamw_update.argtypes = [C.POINTER(AdamWDesc), C.POINTER(AdamWTensor)] + [vp] * 5 + [sz, vp]
         L.janus_trace_begin.argtypes = []
         L.janus_trace_end.argtypes = [C.POINTER(TraceStat), i32, C.POINTER(C.c_int32)]
         for name in EXPORTS:
@@ -532,6 +565,45 @@ def janus_policy_loss(desc: PolicyDesc, logits, actions, old_logp=None, adv=None
     _check(st, "janus_policy_loss")
 
 
+# ---------------------------------------------------------------- layer norm
+def janus_layer_norm_workspace_bytes(desc: NormDesc) -> int:
+    return int(lib().janus_layer_norm_workspace_bytes(C.byref(desc)))
+
+
+def janus_layer_norm_fwd(desc: NormDesc, x, gamma, beta, y, r=None, h=None, mean=None, rstd=None, stream=None):
+    """y of the rows x, or of h = x + r with a residual ``r``; ``mean`` and
+    ``rstd`` (and ``h``) are what the backward reads."""
+    st = lib().janus_layer_norm_fwd(C.byref(desc), _p(x), _p(r), _p(gamma), _p(beta), _p(h), _p(y), _p(mean), _p(rstd),
+                                    _stream(stream))
+    _check(st, "janus_layer_norm_fwd")
+
+
+def janus_layer_norm_bwd(desc: NormDesc, h, gamma, mean, rstd, dy, dx, ws=None, dgamma=None, dbeta=None, dh=None,
+                         stream=None):
+    """``h``: the rows that were normalised (the forward's h, or its x without
+    a residual); ``dh``: the gradient they have from elsewhere."""
+    st = lib().janus_layer_norm_bwd(C.byref(desc), _p(h), _p(gamma), _p(mean), _p(rstd), _p(dy), _p(dh), _p(dx),
+                                    _p(dgamma), _p(dbeta), _p(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                    _stream(stream))
+    _check(st, "janus_layer_norm_bwd")
+
+
+# ---------------------------------------------------------------- drawing tokens
+def janus_sample_workspace_bytes(desc: SampleDesc) -> int:
+    return int(lib().janus_sample_workspace_bytes(C.byref(desc)))
+
+
+def janus_sample(desc: SampleDesc, logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logp=None,
+                 draw_logp=None, kept=None, ws=None, stream=None):
+    """A token of each row by the uniform numbers ``u``; ``temperature``,
+    ``top_k``, ``top_p`` and ``min_p``: device tensors with a setting a row, or
+    None for the descriptor's."""
+    st = lib().janus_sample(C.byref(desc), _p(logits), _p(u), _p(temperature), _p(top_k), _p(top_p), _p(min_p),
+                            _p(tokens), _p(logp), _p(draw_logp), _p(kept), _p(ws),
+                            0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "janus_sample")
+
+
 # ---------------------------------------------------------------- update
 def sgd_workspace_bytes(desc: SgdDesc) -> int:
     return int(lib().janus_sgd_workspace_bytes(C.byref(desc)))
@@ -561,6 +633,36 @@ def janus_sgd_clip_update_noalloc(desc: SgdDesc, params, grads, stats=None, stre
     st = lib().janus_sgd_clip_update_noalloc(C.byref(desc), _ptr_array(params), _ptr_array(grads), S, _p(stats),
                                              None if hold is None else C.c_void_p(int(hold)), _stream(stream))
     _check(st, "janus_sgd_clip_update_noalloc")
+
+
+def adamw_tensors(params, grads, m, v, scale=None, master=None, decay=0.0) -> C.Array:
+    """The tensors of janus_adamw_update, as it takes them: lists of device
+    tensors (``scale`` of 8-bit states; ``master`` with None where a parameter has
+    none), ``decay`` one number or one for each.  Made once for an update's every step;
+    the device tensors have to outlive it."""
+    import torch
+    n = len(params)
+    out = (AdamWTensor * n)()
+    for i in range(n):
+        w = None if master is None else master[i]
+        out[i] = AdamWTensor(_p(params[i]), _p(grads[i]), _p(m[i]), _p(v[i]), None if scale is None else _p(scale[i]), _p(w),
+                             params[i].numel(), float(decay if np.isscalar(decay) else decay[i]),
+                             BF16 if params[i].dtype == torch.bfloat16 else F32)
+    return out
+
+
+def janus_adamw_workspace_bytes(desc: AdamWDesc) -> int:
+    return int(lib().janus_adamw_workspace_bytes(C.byref(desc)))
+
+
+def janus_adamw_update(desc: AdamWDesc, tensors: C.Array, step, lr=None, stats=None, ws=None, stream=None, hold=None):
+    """One AdamW step on ``tensors`` (adamw_tensors); ``step`` an int64 device
+    tensor that counts the steps taken, ``lr`` a float32 device tensor or None
+    for the descriptor's, ``hold`` as in janus_sgd_clip_update."""
+    st = lib().janus_adamw_update(C.byref(desc), tensors, _p(step), _p(lr), _p(stats),
+                                  None if hold is None else C.c_void_p(int(hold)), _p(ws),
+                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "janus_adamw_update")
 
 
 # ---------------------------------------------------------------- tracing
