@@ -22,7 +22,7 @@ namespace {
 
 struct NormArgs {
     int32_t rows, D;
-    float eps, inv_D;
+    float eps, width;      // D as a float: sums are divided by it (the mean of a constant row is its value)
     int64_t ldx, ldh, ldy;
     const void *x, *r;     // (backward: x is h)
     const float *gamma, *beta;
@@ -134,14 +134,14 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
 #pragma unroll
             for (int j = 0; j < VEC; ++j) s[0] += v[i][j];
         row_sum<LANES>(s, red);
-        const float mean = s[0] * a.inv_D;
+        const float mean = s[0] / a.width;
 #pragma unroll
         for (int i = 0; i < P; ++i)
             if ((tid + i * LANES) * VEC < a.D)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) q[0] = fmaf(v[i][j] - mean, v[i][j] - mean, q[0]);
         row_sum<LANES>(q, red);
-        const float rstd = 1.f / sqrtf(q[0] * a.inv_D + a.eps);
+        const float rstd = 1.f / sqrtf(q[0] / a.width + a.eps);
         if (tid == 0 && there) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
@@ -163,14 +163,14 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
             for (int j = 0; j < VEC; ++j) s[0] += v[j];
         }
         row_sum<LANES>(s, red);
-        const float mean = s[0] * a.inv_D;
+        const float mean = s[0] / a.width;
         for (int64_t c = int64_t(tid) * VEC; c < end; c += LANES * VEC) {
             load(c, v);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) q[0] = fmaf(v[j] - mean, v[j] - mean, q[0]);
         }
         row_sum<LANES>(q, red);
-        const float rstd = 1.f / sqrtf(q[0] * a.inv_D + a.eps);
+        const float rstd = 1.f / sqrtf(q[0] / a.width + a.eps);
         if (tid == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_bwd_
             }
             row_sum<LANES>(s, red);
             if (!a.dx || !there) continue;
-            const float m0 = s[0] * a.inv_D, m1 = s[1] * a.inv_D;
+            const float m0 = s[0] / a.width, m1 = s[1] / a.width;
             T* dx = static_cast<T*>(a.dx) + row * a.ldx;
             const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.ldh : nullptr;
 #pragma unroll
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_bwd_
             for (int j = 0; j < VEC; ++j) s[0] += g[j], s[1] = fmaf(g[j], xh[j], s[1]);
         }
         row_sum<LANES>(s, red);
-        const float m0 = s[0] * a.inv_D, m1 = s[1] * a.inv_D;
+        const float m0 = s[0] / a.width, m1 = s[1] / a.width;
         for (int64_t c = int64_t(tid) * VEC; c < end; c += LANES * VEC) {
             load(c);
             float o[VEC];
@@ -402,7 +402,7 @@ bool norm_built(const janus_norm_desc* d) {
 
 NormArgs norm_args(const janus_norm_desc* d) {
     NormArgs a{};
-    a.rows = d->rows, a.D = d->D, a.eps = d->eps, a.inv_D = float(1.0 / d->D);
+    a.rows = d->rows, a.D = d->D, a.eps = d->eps, a.width = float(d->D);
     a.ldx = d->ldx ? d->ldx : d->D, a.ldh = d->ldh ? d->ldh : d->D, a.ldy = d->ldy ? d->ldy : d->D;
     return a;
 }

@@ -351,7 +351,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         lse = __builtin_amdgcn_logf(e);
         __syncthreads();
     }
-    auto logp_of = [&](float x) { return ((x - m) * kLog2e - lse) * kLn2; };
+    auto logp_of = [&](float x) { return fmaf(-lse, kLn2, x - m); };   // (lse: a binary logarithm)
 
     if (temp == 0.f) {   // the first of the largest
         const int j = s.nth(key_of(m), 1);

@@ -252,6 +252,21 @@ def _stream(stream=None) -> Optional[int]:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _stream_of(where: str, stream, *tensors) -> Optional[int]:
+    """The given stream, or the current one, which the tensors (None aside) have
+    to be on the device of: a kernel that got a host tensor's address would fault."""
+    if stream is not None:
+        return stream
+    devices = {t.get_device() for t in tensors if t is not None}
+    if -1 in devices:
+        raise ValueError(f"{where}: a tensor is not on the GPU")
+    import torch
+    now = torch.cuda.current_device()
+    if devices - {now}:
+        raise ValueError(f"{where}: tensors on the devices {sorted(devices)}, the current device is {now}")
+    return torch._C._cuda_getCurrentRawStream(now)
+
+
 def _ptr_array(tensors: Sequence) -> C.Array:
     arr = (C.c_void_p * len(tensors))()
     for i, t in enumerate(tensors):
@@ -574,7 +589,7 @@ def janus_layer_norm_fwd(desc: NormDesc, x, gamma, beta, y, r=None, h=None, mean
     """y of the rows x, or of h = x + r with a residual ``r``; ``mean`` and
     ``rstd`` (and ``h``) are what the backward reads."""
     st = lib().janus_layer_norm_fwd(C.byref(desc), _p(x), _p(r), _p(gamma), _p(beta), _p(h), _p(y), _p(mean), _p(rstd),
-                                    _stream(stream))
+                                    _stream_of("janus_layer_norm_fwd", stream, x, r, gamma, beta, h, y, mean, rstd))
     _check(st, "janus_layer_norm_fwd")
 
 
@@ -584,7 +599,8 @@ def janus_layer_norm_bwd(desc: NormDesc, h, gamma, mean, rstd, dy, dx, ws=None, 
     a residual); ``dh``: the gradient they have from elsewhere."""
     st = lib().janus_layer_norm_bwd(C.byref(desc), _p(h), _p(gamma), _p(mean), _p(rstd), _p(dy), _p(dh), _p(dx),
                                     _p(dgamma), _p(dbeta), _p(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                    _stream(stream))
+                                    _stream_of("janus_layer_norm_bwd", stream, h, gamma, mean, rstd, dy, dh, dx, dgamma, dbeta,
+                                               ws))
     _check(st, "janus_layer_norm_bwd")
 
 
@@ -600,7 +616,9 @@ def janus_sample(desc: SampleDesc, logits, u, tokens, temperature=None, top_k=No
     None for the descriptor's."""
     st = lib().janus_sample(C.byref(desc), _p(logits), _p(u), _p(temperature), _p(top_k), _p(top_p), _p(min_p),
                             _p(tokens), _p(logp), _p(draw_logp), _p(kept), _p(ws),
-                            0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+                            0 if ws is None else ws.numel() * ws.element_size(),
+                            _stream_of("janus_sample", stream, logits, u, temperature, top_k, top_p, min_p, tokens, logp,
+                                       draw_logp, kept, ws))
     _check(st, "janus_sample")
 
 
@@ -638,8 +656,7 @@ def janus_sgd_clip_update_noalloc(desc: SgdDesc, params, grads, stats=None, stre
 def adamw_tensors(params, grads, m, v, scale=None, master=None, decay=0.0) -> C.Array:
     """The tensors of janus_adamw_update, as it takes them: lists of device
     tensors (``scale`` of 8-bit states; ``master`` with None where a parameter has
-    none), ``decay`` one number or one for each.  Made once for an update's every step;
-    the device tensors have to outlive it."""
+    none), ``decay`` one number or one for each.  Made once for an update's every step."""
     import torch
     n = len(params)
     out = (AdamWTensor * n)()
@@ -648,6 +665,10 @@ def adamw_tensors(params, grads, m, v, scale=None, master=None, decay=0.0) -> C.
         out[i] = AdamWTensor(_p(params[i]), _p(grads[i]), _p(m[i]), _p(v[i]), None if scale is None else _p(scale[i]), _p(w),
                              params[i].numel(), float(decay if np.isscalar(decay) else decay[i]),
                              BF16 if params[i].dtype == torch.bfloat16 else F32)
+    out.tensors = [t for ts in (params, grads, m, v, scale or [], master or []) for t in ts if t is not None]   # (kept alive)
+    devices = {t.get_device() for t in out.tensors}
+    if len(devices) > 1:
+        raise ValueError(f"adamw_tensors: tensors on the devices {sorted(devices)}")
     return out
 
 
@@ -661,7 +682,8 @@ def janus_adamw_update(desc: AdamWDesc, tensors: C.Array, step, lr=None, stats=N
     for the descriptor's, ``hold`` as in janus_sgd_clip_update."""
     st = lib().janus_adamw_update(C.byref(desc), tensors, _p(step), _p(lr), _p(stats),
                                   None if hold is None else C.c_void_p(int(hold)), _p(ws),
-                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+                                  0 if ws is None else ws.numel() * ws.element_size(),
+                                  _stream_of("janus_adamw_update", stream, step, lr, stats, ws, *getattr(tensors, "tensors", ())[:1]))
     _check(st, "janus_adamw_update")
 
 

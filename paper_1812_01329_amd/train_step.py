@@ -8,7 +8,8 @@ reverse).  All arithmetic happens inside libjanus.so.
 """
 from __future__ import annotations
 
-from typing import Dict, Optional, Sequence, Tuple
+import dataclasses
+from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import numpy as np
 import torch
@@ -55,15 +56,88 @@ class SgdUpdate:
         J.janus_sgd_clip_update(self.desc, self.params, self.grads, stats=self.stats, ws=self.ws, hold=hold)
 
 
+@dataclasses.dataclass
+class AdamW:
+    """An ``update`` of the training steps in the place of (lr, max_norm):
+    AdamW with states of 32 or 8 bits.  ``decay`` is for the matrices (vectors,
+    biases and norms' scales among them, have none); ``masters`` keeps float32
+    copies of bf16 parameters."""
+    lr: float
+    max_norm: float = 0.0
+    betas: Tuple[float, float] = (0.9, 0.999)
+    eps: float = 1e-8
+    decay: float = 0.0
+    bits: int = 32
+    masters: bool = False
+    seed: int = 0
+
+
+class AdamWUpdate:
+    """The AdamW update that ends a training step (janus_adamw_update): every
+    parameter tensor with its float32 gradient, float32 and bf16 parameters in one
+    call under one norm."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], spec: AdamW):
+        if spec.bits not in (8, 32):
+            raise ValueError(f"states have 8 or 32 bits, not {spec.bits}")
+        for p, g in zip(params, grads):
+            if p.dtype not in (torch.float32, torch.bfloat16) or g.dtype != torch.float32 or p.numel() != g.numel():
+                raise ValueError("parameters are float32 or bf16, their gradients float32 of the same size")
+        q = spec.bits == 8
+        dev, n = params[0].device, len(params)
+        zeros = lambda p: torch.zeros(p.numel(), dtype=torch.uint8 if q else torch.float32, device=dev)
+        self.spec = spec
+        self.params, self.grads = [p.view(-1) for p in params], [g.view(-1) for g in grads]
+        self.m, self.v = [zeros(p) for p in params], [zeros(p) for p in params]
+        self.scale = [torch.zeros(-(-p.numel() // 256), 2, device=dev) for p in params] if q else None
+        self.master = [p.float() if spec.masters and p.dtype == torch.bfloat16 else None for p in self.params]
+        self.step = torch.zeros(1, dtype=torch.int64, device=dev)
+        self.stats = torch.zeros(2, dtype=torch.float32, device=dev)   # [norm before clipping, scale]
+        self.desc = J.AdamWDesc(n, J.ADAMW_8BIT if q else J.ADAMW_F32, spec.lr, *spec.betas, spec.eps, spec.max_norm,
+                                spec.seed)
+        self.tensors = J.adamw_tensors(self.params, self.grads, self.m, self.v, self.scale, self.master,
+                                       [spec.decay if p.dim() > 1 else 0.0 for p in params])
+        self.ws = torch.empty(J.janus_adamw_workspace_bytes(self.desc), dtype=torch.uint8, device=dev)
+
+    def apply(self, hold: Optional[int] = None, lr: Optional[torch.Tensor] = None):
+        """``hold`` as in SgdUpdate.apply; ``lr``: a float32 device tensor
+        that is read when the update runs, in the spec's place."""
+        J.janus_adamw_update(self.desc, self.tensors, self.step, lr=lr, stats=self.stats, ws=self.ws, hold=hold)
+
+    def state_dict(self) -> Dict[str, List[torch.Tensor]]:
+        """Copies of what the update keeps between steps."""
+        kept = dict(m=self.m, v=self.v, scale=self.scale or [], master=[w for w in self.master if w is not None],
+                    step=[self.step])
+        return {k: [t.clone() for t in v] for k, v in kept.items()}
+
+    def load_state_dict(self, state: Dict[str, List[torch.Tensor]]):
+        """Takes a state_dict over, into the tensors that the update works on."""
+        mine = dict(m=self.m, v=self.v, scale=self.scale or [], master=[w for w in self.master if w is not None],
+                    step=[self.step])
+        for k, ts in mine.items():
+            if [(t.shape, t.dtype) for t in ts] != [(t.shape, t.dtype) for t in state[k]]:
+                raise ValueError(f"the state's {k} are those of other parameters or bits")
+        for k, ts in mine.items():
+            for t, new in zip(ts, state[k]):
+                t.copy_(new)
+
+
+def make_update(params, grads, update):
+    """The update of an ``update`` argument: (lr, max_norm) or an AdamW."""
+    if isinstance(update, AdamW):
+        return AdamWUpdate(params, grads, update)
+    return SgdUpdate(params, grads, *update)
+
+
 class LSTMStep:
     """Device state and call sequence of an LSTM training step.
 
     ``skip_dx``: do not form the gradient of the (non-embedding) input x,
     as in the regression workload where x is data.  ``update`` = (lr,
-    max_norm) appends the parameter update to the step."""
+    max_norm) or an AdamW appends the parameter update to the step."""
 
     def __init__(self, w: wl.LSTMWorkload, device="cuda", skip_dx: Optional[bool] = None,
-                 update: Optional[Tuple[float, float]] = None):
+                 update: Union[Tuple[float, float], AdamW, None] = None):
         self.w = w
         self.device = device
         tdt = _tdt(w.dtype)
@@ -129,7 +203,7 @@ class LSTMStep:
         self.update = None
         if update is not None:
             P, G = self.parameters()
-            self.update = SgdUpdate(P, G, *update)
+            self.update = make_update(P, G, update)
         # the timeout word of the step's recurrences: a step whose forward or
         # backward wait ran out leaves the parameters unchanged
         self.fault = J.janus_lstm_fault_flag(self.desc, self.ws)
@@ -204,7 +278,7 @@ class LSTMStep:
 class TreeStep:
     """Device state and call sequence of a TreeLSTM training step."""
 
-    def __init__(self, w: wl.TreeWorkload, device="cuda", update: Optional[Tuple[float, float]] = None):
+    def __init__(self, w: wl.TreeWorkload, device="cuda", update: Union[Tuple[float, float], AdamW, None] = None):
         self.w = w
         self.device = device
         f = torch.float32
@@ -234,8 +308,8 @@ class TreeStep:
                                dtype=torch.uint8, device=device)
         self.update = None
         if update is not None:
-            self.update = SgdUpdate([self.emb, self.W, self.U, self.b, self.Ws, self.bs],
-                                    [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], *update)
+            self.update = make_update([self.emb, self.W, self.U, self.b, self.Ws, self.bs],
+                                      [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], update)
 
     def run(self):
         w = self.w
@@ -258,7 +332,7 @@ class TreeStep:
 class TreeRNNStep:
     """Device state and call sequence of a TreeRNN training step."""
 
-    def __init__(self, w: wl.TreeRNNWorkload, device="cuda", update: Optional[Tuple[float, float]] = None):
+    def __init__(self, w: wl.TreeRNNWorkload, device="cuda", update: Union[Tuple[float, float], AdamW, None] = None):
         self.w = w
         self.device = device
         f = torch.float32
@@ -286,8 +360,8 @@ class TreeRNNStep:
                                dtype=torch.uint8, device=device)
         self.update = None
         if update is not None:
-            self.update = SgdUpdate([self.emb, self.W, self.b, self.Ws, self.bs],
-                                    [self.demb, self.dW, self.db, self.dWs, self.dbs], *update)
+            self.update = make_update([self.emb, self.W, self.b, self.Ws, self.bs],
+                                      [self.demb, self.dW, self.db, self.dWs, self.dbs], update)
 
     def run(self):
         w = self.w
@@ -309,7 +383,7 @@ class TreeRNNStep:
 class ChildSumStep:
     """Device state and call sequence of a Child-Sum TreeLSTM training step."""
 
-    def __init__(self, w: wl.ChildSumWorkload, device="cuda", update: Optional[Tuple[float, float]] = None):
+    def __init__(self, w: wl.ChildSumWorkload, device="cuda", update: Union[Tuple[float, float], AdamW, None] = None):
         self.w = w
         self.device = device
         f = torch.float32
@@ -339,8 +413,8 @@ class ChildSumStep:
                                dtype=torch.uint8, device=device)
         self.update = None
         if update is not None:
-            self.update = SgdUpdate([self.emb, self.W, self.U, self.b, self.Ws, self.bs],
-                                    [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], *update)
+            self.update = make_update([self.emb, self.W, self.U, self.b, self.Ws, self.bs],
+                                      [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], update)
 
     def run(self):
         w = self.w
@@ -360,9 +434,9 @@ class ChildSumStep:
                     dWs=_f64(self.dWs), dbs=_f64(self.dbs))
 
 
-def make_step(w, device="cuda", update: Optional[Tuple[float, float]] = None):
+def make_step(w, device="cuda", update: Union[Tuple[float, float], AdamW, None] = None):
     """The training step of a workload; ``update`` = (lr, max_norm) appends
-    the SGD update with global-norm clipping."""
+    the SGD update with global-norm clipping, an AdamW that update."""
     if isinstance(w, wl.TreeRNNWorkload):
         return TreeRNNStep(w, device, update=update)
     if isinstance(w, wl.ChildSumWorkload):

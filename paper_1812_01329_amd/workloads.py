@@ -437,22 +437,30 @@ class PolicyWorkload:
     tokens: np.ndarray     # [T + 1, B] int32
     adv: np.ndarray        # [B] float32, one advantage a sequence
     params: Dict[str, np.ndarray]
+    norm: bool = False     # norms around the layer, on a residual stream
 
 
-def sequence_policy(V=1000, M=128, D=256, N=16, K=4, R=8, B=8, T=24, dtype=F32, seed=None) -> PolicyWorkload:
+def sequence_policy(V=1000, M=128, D=256, N=16, K=4, R=8, B=8, T=24, dtype=F32, seed=None, norm=False) -> PolicyWorkload:
     """Token policy of one convolution and selective-scan layer: lengths uniform
     in [1, T], Zipf(1.1) tokens, advantages N(0, 1); products' weights U(-a, a)
     with a = 1/sqrt(width), decay rates 1..N, step sizes log-uniform in
-    [0.001, 0.1] through the bias."""
+    [0.001, 0.1] through the bias.  ``norm``: a norm before the layer and one after
+    its residual sum, scales U(0.5, 1.5), shifts U(-0.1, 0.1), and the product back
+    to the embedding's width, which the logits are then formed from."""
     rp, _, rl, rt = _streams(7, seed)
     w = lambda *s: _round_if(uniform(rp, 1.0 / np.sqrt(s[-1]), s), dtype)
     d0 = np.exp(rp.uniform(np.log(1e-3), np.log(1e-1), D))
     params = dict(E=w(V, M), Win=w(2 * D, M), conv_w=w(D, K), conv_b=w(D), Wx=w(R + 2 * N, D), Wdt=w(D, R),
                   Wout=w(V, D), A=-np.tile(np.arange(1, N + 1, dtype=np.float32), (D, 1)),
                   Dskip=np.ones(D, np.float32), dt_bias=(d0 + np.log(-np.expm1(-d0))).astype(np.float32))
+    if norm:
+        params.update(Wo=w(M, D), Wout=w(V, M))
+        for k in "01":
+            params["norm_g" + k] = rp.uniform(0.5, 1.5, M).astype(np.float32)
+            params["norm_b" + k] = rp.uniform(-0.1, 0.1, M).astype(np.float32)
     lengths = rl.integers(1, T + 1, size=B).astype(np.int32)
     tokens = zipf_truncated(rt, 1.1, V, (T + 1, B))
-    return PolicyWorkload("policy", dtype, V, M, D, N, K, R, B, T, lengths, tokens, normal(rt, (B,)), params)
+    return PolicyWorkload("policy", dtype, V, M, D, N, K, R, B, T, lengths, tokens, normal(rt, (B,)), params, norm)
 
 
 # Named full-size workloads, in the order of the five configurations.

@@ -1,0 +1,271 @@
+"""GPU parity of the layer norm (janus_layer_norm_*) against the float64 oracle:
+widths from 1 to past what registers hold, any alignment and row stride, the
+residual sum and its gradient, in place, rows with NaN beside others.
+
+Tolerances.  A row's sums are taken over at most 64 serial and 20 tree additions of
+float32: the mean is off by at most 84 * 2^-24 = 5e-6 of the mean |h|, which is here
+at most about the deviation, as are the variance and rstd (relative): y by 1e-5 of
+its largest and dx, with three more such sums, by 2e-5.  bf16 results are rounded
+once more: 2^-8 of themselves.  dgamma and dbeta add up rows / 256 + 64 terms a lane and
+tree: each entry within (rows / 256 + 64) * 2^-24 + 1e-5 of the sum of its terms' magnitudes."""
+import numpy as np
+import pytest
+
+from oracle import norm as oracle
+
+pytestmark = pytest.mark.gpu
+
+
+def tens(torch, a, dt, ld, shift):
+    """The rows `a` in a buffer with row stride ld, `shift` elements off its
+    start; NaN between the rows (never to be read or written)."""
+    R, D = a.shape
+    flat = torch.full((max(R, 1) * ld + shift + 8,), float("nan"), dtype=dt, device="cuda")
+    t = flat[shift:shift + R * ld].view(R, ld)[:, :D]
+    t.copy_(torch.from_numpy(a))
+    return t
+
+
+class Case:
+    def __init__(self, rows, D, dtype="f32", pads=(0, 0, 0), shift=0, residual=False, affine=True, seed=0, offset=0.0):
+        import torch
+        from paper_1812_01329_amd import janus as J
+        rng = np.random.default_rng(seed * 1000003 + rows * 1009 + D)
+        self.J, self.torch, self.rows, self.D = J, torch, rows, D
+        self.dt = torch.float32 if dtype == "f32" else torch.bfloat16
+        ld = [D + p for p in pads]
+        lds = [l if p else 0 for l, p in zip(ld, pads)]
+        if not residual:
+            lds[1] = lds[0]
+            ld[1] = ld[0]
+        self.desc = J.NormDesc(rows, D, J.F32 if dtype == "f32" else J.BF16, 1e-5, *lds)
+        mk = lambda s=1.0, o=0.0: (rng.normal(size=(rows, D)) * s + o).astype(np.float32)
+        T = lambda a, i: tens(torch, a, self.dt, ld[i], shift)
+        self.x, self.dy = T(mk(1.0, offset), 0), T(mk(), 2)
+        self.r = T(mk(1.5, 0.2), 1) if residual else None
+        self.dh = T(mk(), 1) if residual else None
+        self.y, self.dx = T(mk() * 0, 2), T(mk() * 0, 0)
+        self.h = T(mk() * 0, 1) if residual else None
+        f = lambda a: torch.from_numpy(a.astype(np.float32)).cuda()
+        self.gamma = f(rng.uniform(0.5, 1.5, D)) if affine else None
+        self.beta = f(rng.normal(0, 0.2, D)) if affine else None
+        n = lambda *s: torch.full(s, float("nan"), device="cuda")
+        self.mean, self.rstd, self.dgamma, self.dbeta = n(rows), n(rows), n(D), n(D)
+        self.ws = torch.empty(max(1, J.janus_layer_norm_workspace_bytes(self.desc)), dtype=torch.uint8, device="cuda")
+
+    def forward(self, **kw):
+        a = dict(r=self.r, h=self.h, mean=self.mean, rstd=self.rstd)
+        a.update(kw)
+        self.J.janus_layer_norm_fwd(self.desc, self.x, self.gamma, self.beta, a.pop("y", self.y), **a)
+
+    def backward(self, **kw):
+        a = dict(dgamma=self.dgamma, dbeta=self.dbeta, dh=self.dh)
+        a.update(kw)
+        self.J.janus_layer_norm_bwd(self.desc, self.x if self.h is None else self.h, self.gamma, self.mean, self.rstd, self.dy,
+                                    a.pop("dx", self.dx), self.ws, **a)
+
+    def sums(self):
+        h = self.x.float()
+        return h if self.r is None else (h + self.r.float()).to(self.dt).float()
+
+    def check(self, back=True):
+        np64 = lambda t: None if t is None else t.detach().double().cpu().numpy()
+        h = np64(self.sums())
+        if self.h is not None:
+            assert self.torch.equal(self.h.float(), self.sums())
+        y, mean, rstd = oracle.forward(h, np64(self.gamma), np64(self.beta))
+        bf = 2.0 ** -8 if self.dt == self.torch.bfloat16 else 0.0
+        got = np64(self.y)
+        size = np.abs(y).max()
+        assert (np.abs(got - y) <= bf * np.abs(y) + 1e-5 * size).all(), np.abs(got - y).max() / size
+        assert np.abs(np64(self.mean) - mean).max() <= 5e-6 * max(np.abs(h).mean(1).max(), 1e-6)
+        assert (np.abs(np64(self.rstd) - rstd) <= 1e-5 * rstd).all()
+        if not back:
+            return
+        dy = np64(self.dy)
+        dx, dg, db = oracle.backward(h, dy, np64(self.gamma), np64(self.dh))
+        size = max(np.abs(dx).max(), (np.abs(dy) * (1 if self.gamma is None else np64(self.gamma)) * rstd[:, None]).max())
+        got = np64(self.dx)
+        assert (np.abs(got - dx) <= bf * np.abs(dx) + 2e-5 * size).all(), np.abs(got - dx).max() / size
+        xh = (h - mean[:, None]) * rstd[:, None]
+        tol = (self.rows / 256 + 64) * 2.0 ** -24 + 1e-5
+        if self.dgamma is not None:
+            assert (np.abs(np64(self.dgamma) - dg) <= tol * (np.abs(dy) * (np.abs(xh) + 1)).sum(0) + 1e-30).all()
+            assert (np.abs(np64(self.dbeta) - db) <= tol * np.abs(dy).sum(0) + 1e-30).all()
+
+
+SHAPES = [(1, 1), (3, 2), (5, 7), (2, 16), (17, 31), (33, 64), (9, 100), (4, 127), (21, 128), (19, 256), (65, 301), (3, 511),
+          (6, 512), (11, 1024), (7, 1300), (13, 2048), (5, 2049), (2, 4100), (9, 8192), (1, 20000), (3, 32768), (2, 40001),
+          (2, 65544), (5000, 8), (3001, 40), (1500, 650)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,D", SHAPES)
+def test_dense(rows, D, dtype):
+    print(f"[norm] {rows}x{D} {dtype}", flush=True)
+    for residual in (False, True):
+        c = Case(rows, D, dtype, residual=residual)
+        c.forward()
+        c.backward()
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pads,shift", [((1, 1, 1), 0), ((0, 2, 8), 1), ((8, 8, 8), 8), ((4, 4, 4), 4), ((2, 6, 2), 2),
+                                        ((300, 0, 16), 3)])
+@pytest.mark.parametrize("D", [24, 301, 1024, 9000])
+def test_strides_and_alignment(D, pads, shift, dtype):
+    """Every access width, rows that start anywhere; what lies between the rows is
+    neither read (it is NaN) nor written."""
+    print(f"[norm strides] {D} {pads} {shift} {dtype}", flush=True)
+    for residual in (False, True):
+        c = Case(7, D, dtype, pads, shift, residual)
+        c.forward()
+        c.backward()
+        c.check()
+        for t in (c.y, c.dx, c.h):
+            if t is not None and t.stride(0) > D:
+                gap = t.as_strided((6, t.stride(0) - D), (t.stride(0), 1), t.storage_offset() + D)
+                assert bool(gap.isnan().all())
+
+
+@pytest.mark.parametrize("D", [40, 512, 5000, 70000])
+def test_optional_parts_and_in_place(D):
+    import torch
+    print(f"[norm in place] {D}", flush=True)
+    c = Case(6, D, "bf16", affine=False)
+    c.forward()
+    c.backward()
+    c.check()
+    full = c.dx.clone()
+    c.dx.zero_()
+    c.backward(dgamma=None, dbeta=None)
+    assert torch.equal(c.dx, full)
+    g, b = c.dgamma.clone(), c.dbeta.clone()
+    c.dgamma.zero_()
+    c.backward(dx=None, dbeta=None)
+    assert torch.equal(c.dgamma, g)
+    c.dbeta.zero_()
+    c.backward(dx=None, dgamma=None)
+    assert torch.equal(c.dbeta, b)
+    # the sum in the residual's place, in x's place, or not wanted; dx in dh's place
+    c = Case(6, D, "bf16", residual=True)
+    c.forward()
+    c.backward()
+    c.check()
+    for where in ("r", "x"):
+        keep = getattr(c, where).clone()
+        y = torch.empty_like(c.y)
+        c.forward(y=y, h=getattr(c, where))
+        assert torch.equal(getattr(c, where), c.h) and torch.equal(y, c.y)
+        getattr(c, where).copy_(keep)
+    y = torch.empty_like(c.y)
+    c.forward(y=y, h=None, mean=None, rstd=None)
+    assert torch.equal(y, c.y)
+    into = c.dh.clone()
+    c.backward(dx=into, dh=into)
+    assert torch.equal(into, c.dx)
+
+
+@pytest.mark.parametrize("D", [33, 700, 5000, 40000])
+def test_rows_do_not_touch_each_other(D):
+    """A row with NaN, one with an infinity: their y and dx are NaN, the others'
+    are what they are without them."""
+    import torch
+    c = Case(9, D, "f32")
+    c.forward()
+    c.backward()
+    y, dx = c.y.clone(), c.dx.clone()
+    c.x[2, D // 2] = float("nan")
+    c.x[5, 0] = float("inf")
+    c.forward()
+    c.backward()
+    bad = torch.tensor([2, 5], device="cuda")
+    good = torch.tensor([0, 1, 3, 4, 6, 7, 8], device="cuda")
+    assert torch.equal(c.y[good], y[good]) and torch.equal(c.dx[good], dx[good])
+    assert bool(c.y[bad].isnan().all()) and bool(c.dx[bad].isnan().all())
+    assert bool(c.dgamma.isnan().all()) and bool(c.dbeta.isfinite().all())
+
+
+def test_constant_rows_and_large_means():
+    """A constant row has y = beta; a mean 1000 deviations away costs the bits it
+    has in common: 1000 * 2^-24 * 84 = 5e-3 of the deviation."""
+    import torch
+    c = Case(4, 600, "f32")
+    c.x.fill_(3.25)
+    c.forward()
+    c.backward()
+    assert torch.equal(c.y, c.beta.expand(4, 600))
+    assert bool(c.dx.isfinite().all())
+    c = Case(4, 600, "f32", offset=1000.0)
+    c.forward()
+    y = oracle.forward(c.x.double().cpu().numpy(), c.gamma.double().cpu().numpy(), c.beta.double().cpu().numpy())[0]
+    assert np.abs(c.y.double().cpu().numpy() - y).max() <= 5e-3 * np.abs(y).max()
+
+
+def test_no_rows():
+    import torch
+    from paper_1812_01329_amd import janus as J
+    d = J.NormDesc(0, 300, J.F32, 1e-5, 0, 0, 0)
+    g, b = torch.full((300,), 7.0, device="cuda"), torch.full((300,), 7.0, device="cuda")
+    J.janus_layer_norm_fwd(d, None, None, None, None)
+    J.janus_layer_norm_bwd(d, None, None, None, None, None, None, dgamma=g, dbeta=b)
+    assert not bool(g.any()) and not bool(b.any())
+
+
+def test_many_rows_repeat_bit_for_bit():
+    """Sums over many rows (more than workgroups take at once) are taken in a fixed order."""
+    import torch
+    c = Case(70001, 24, "f32")
+    c.forward()
+    c.backward()
+    c.check()
+    g, b, dx = c.dgamma.clone(), c.dbeta.clone(), c.dx.clone()
+    for _ in range(3):
+        c.backward()
+        assert torch.equal(c.dgamma, g) and torch.equal(c.dbeta, b) and torch.equal(c.dx, dx)
+
+
+def test_gradients_against_differences():
+    """dx, dgamma and dbeta by central differences of the kernel's own float32
+    forward: step 2^-5, y's error 1e-5, the third derivative's part 2^-10 / 6: 5e-3."""
+    import torch
+    c = Case(2, 12, "f32", residual=True)
+    c.forward()
+    c.backward()
+    w, wh = c.dy.double(), c.dh.double()
+
+    def loss():
+        c.forward()
+        return float((c.y.double() * w).sum() + (c.h.double() * wh).sum())
+
+    for t, g in ((c.x, c.dx), (c.r, c.dx), (c.gamma[None], c.dgamma[None]), (c.beta[None], c.dbeta[None])):
+        for i in range(t.shape[0]):
+            for j in range(t.shape[1]):
+                keep = float(t[i, j])
+                t[i, j] = keep + 2.0 ** -5
+                up = loss()
+                t[i, j] = keep - 2.0 ** -5
+                down = loss()
+                t[i, j] = keep
+                assert abs((up - down) * 16 - float(g[i, j])) <= 5e-3 * max(1.0, float(g.abs().max())), (i, j)
+
+
+def test_rows_more_than_2_to_32_elements_apart():
+    import torch
+    from paper_1812_01329_amd import janus as J
+    ld, D = (1 << 32) + 8, 96
+    print("[norm offsets]", flush=True)
+    big = torch.empty(2 * ld + D, dtype=torch.bfloat16, device="cuda")
+    x = big.as_strided((3, D), (ld, 1))
+    x.copy_(torch.randn(3, D, generator=torch.Generator().manual_seed(1)))
+    y, dy = torch.empty(3, D, dtype=torch.bfloat16, device="cuda"), torch.randn(3, D, device="cuda").bfloat16()
+    near, dx, want = x.contiguous(), torch.empty_like(y), torch.empty_like(y)
+    mean, rstd = torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+    far, dense = J.NormDesc(3, D, J.BF16, 1e-5, ld, ld, 0), J.NormDesc(3, D, J.BF16, 1e-5, 0, 0, 0)
+    J.janus_layer_norm_fwd(dense, near, None, None, want, mean=mean, rstd=rstd)
+    J.janus_layer_norm_fwd(far, x, None, None, y, mean=mean, rstd=rstd)
+    assert torch.equal(y, want)
+    J.janus_layer_norm_bwd(dense, near, None, mean, rstd, dy, dx)
+    J.janus_layer_norm_bwd(J.NormDesc(3, D, J.BF16, 1e-5, 0, ld, 0), x, None, mean, rstd, dy, want)
+    assert torch.equal(dx, want)
