@@ -6,9 +6,11 @@
 //
 // Two passes, both bound by memory: the norm has to be known before the first
 // parameter moves (nothing moves when it is not finite), so the gradients are read
-// twice.  Tensors are cut into tiles of 4096 elements, which the workgroups of a
+// twice.  Tensors are cut into tiles of 1024 or 4096 elements, which the workgroups of a
 // launch take in turn; the second pass takes them in the opposite order, for the last
-// gradients of the first one are then still in the 256 MB cache before the HBM.
+// gradients of the first one are then still in the 256 MB cache before the HBM.  A
+// table of the tensors goes to the kernels by value; one of more than 52 is written to the
+// workspace by launches that have a part of it each, and each pass stays one launch.
 //
 // 8-bit states: 256 elements are one access of four a lane in a wave, whose
 // largest the lanes find among themselves.  With E the exponent that makes the largest
@@ -26,24 +28,22 @@ namespace janus {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 4096;      // elements
 constexpr int kBlocks = 1024;    // workgroups a launch at most
-constexpr int kTable = 40;       // tensors a launch
+constexpr int kTable = 52;       // tensors of a table passed by value
+constexpr int kStarts = 1024;    // tensors whose tiles are looked up in LDS
 
-// The tensors of a launch of the first pass, passed by value: tile t belongs to the
-// last tensor that starts at t or before.
-struct NormTable {
-    int n;
-    int64_t tile[kTable + 1];
-    const float* g[kTable];
-    int64_t size[kTable];
-};
-struct AdamTable {
+// Tensors and their tiles: tile t belongs to the last tensor that starts at t or before.
+struct TensorTable {
     int n, first;                // first: the place of tensor 0 in the call
     int64_t tile[kTable + 1];
     janus_adamw_tensor t[kTable];
 };
-static_assert(sizeof(AdamTable) < 3600, "kernel arguments hold 4 KB");
+static_assert(sizeof(TensorTable) < 3800, "kernel arguments hold 4 KB");
+struct Tensors {                 // the same in the workspace
+    int n;
+    const int64_t* tile;
+    const janus_adamw_tensor* t;
+};
 
 // What the first pass leaves for the second, behind the block sums of the norm
 struct Control {
@@ -66,15 +66,27 @@ struct AdamArgs {
     float* stats;
 };
 
+// Tiles' tensors are found by a copy of their starts in LDS; a table passed by value has so
+// few that it is read in its place.
+__device__ __forceinline__ void prepare(const TensorTable&, int64_t*) {}
+__device__ __forceinline__ int64_t start(const TensorTable& t, const int64_t*, int i) { return t.tile[i]; }
+__device__ __forceinline__ void prepare(const Tensors& t, int64_t* lds) {
+    if (t.n <= kStarts)
+        for (int i = threadIdx.x; i <= t.n; i += kThreads) lds[i] = t.tile[i];
+    __syncthreads();
+}
+__device__ __forceinline__ int64_t start(const Tensors& t, const int64_t* lds, int i) {
+    return t.n <= kStarts ? lds[i] : t.tile[i];
+}
 template <typename Table>
-__device__ __forceinline__ int tensor_of(const Table& t, int64_t tile) {
+__device__ __forceinline__ int tensor_of(const Table& t, const int64_t* lds, int64_t tile) {
     int lo = 0, hi = t.n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (t.tile[mid] <= tile) lo = mid;
+        if (start(t, lds, mid) <= tile) lo = mid;
         else hi = mid;
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 // 32 random bits a number
@@ -97,12 +109,21 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
     return s;
 }
 
-// Pass one: a workgroup's sum of squares; the first of the first launch also forms
-// what depends on the step's number alone.
-__global__ __launch_bounds__(kThreads) void adamw_norm_kernel(NormTable t, AdamArgs a, double* sums, bool first) {
+__global__ void adamw_table_kernel(TensorTable v, int64_t* tile, janus_adamw_tensor* t) {
+    const int i = threadIdx.x;
+    if (i <= v.n) tile[v.first + i] = v.tile[i];   // (the next part's first again, or the end)
+    if (i < v.n) t[v.first + i] = v.t[i];
+}
+
+// Pass one: a workgroup's sum of squares; the first one also forms what depends on the
+// step's number alone.
+template <int TILE, typename Table>
+__global__ __launch_bounds__(kThreads) void adamw_norm_kernel(Table t, AdamArgs a) {
     __shared__ double red[kThreads / 64];
+    __shared__ int64_t lds[kStarts + 1];
+    prepare(t, lds);
     const int tid = threadIdx.x;
-    if (first && blockIdx.x == 0 && tid == 0) {
+    if (blockIdx.x == 0 && tid == 0) {
         Control c;
         c.t = *a.step + 1;
         c.lr = a.lr_dev ? *a.lr_dev : a.lr;
@@ -111,31 +132,60 @@ __global__ __launch_bounds__(kThreads) void adamw_norm_kernel(NormTable t, AdamA
         c.key = mix(mix(a.seed) ^ uint32_t(c.t));
         *a.ctl = c;
     }
-    double acc = 0.0;
-    for (int64_t tile = blockIdx.x; tile < t.tile[t.n]; tile += gridDim.x) {
-        const int i = tensor_of(t, tile);
-        const int64_t at = (tile - t.tile[i]) * kTile;
-        const int64_t left = t.size[i] - at;
-        const int len = int(left < kTile ? left : kTile);
-        const float* g = t.g[i] + at;
+    // the next tile is on its way while one is added up
+    constexpr int U = TILE / 4 / kThreads;
+    struct Part {
+        float4 v[U];
+        float edge[2];
+    };
+    auto load = [&](int64_t tile, Part& x) {
+        const int i = tensor_of(t, lds, tile);
+        const int64_t at = (tile - start(t, lds, i)) * TILE;
+        const int64_t left = t.t[i].size - at;
+        const int len = int(left < TILE ? left : TILE);
+        const float* g = t.t[i].g + at;
         // elements before the first 16-byte boundary, then float4s, then the rest
         const int head = min(len, int((16u - (reinterpret_cast<uintptr_t>(g) & 15u)) & 15u) / 4);
         const int n4 = (len - head) / 4;
         const float4* g4 = reinterpret_cast<const float4*>(g + head);
 #pragma unroll
-        for (int u = 0; u < kTile / 4 / kThreads; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int k = tid + u * kThreads;
-            if (k < n4) {
-                const float4 v = g4[k];
-                acc += double(v.x) * v.x + double(v.y) * v.y + double(v.z) * v.z + double(v.w) * v.w;
-            }
+            x.v[u] = k < n4 ? g4[k] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
         const int rest = head + 4 * n4 + tid;
-        if (tid < head) acc += double(g[tid]) * g[tid];
-        if (rest < len) acc += double(g[rest]) * g[rest];
+        x.edge[0] = tid < head ? g[tid] : 0.f;
+        x.edge[1] = rest < len ? g[rest] : 0.f;
+    };
+    double acc = 0.0;
+    auto add = [&](const Part& x) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            acc += double(x.v[u].x) * x.v[u].x + double(x.v[u].y) * x.v[u].y + double(x.v[u].z) * x.v[u].z + double(x.v[u].w) * x.v[u].w;
+        acc += double(x.edge[0]) * x.edge[0] + double(x.edge[1]) * x.edge[1];
+    };
+    const int64_t tiles = start(t, lds, t.n);
+    int64_t tile = blockIdx.x;
+    if (tile < tiles) {
+        Part x, y;
+        load(tile, x);
+        while (true) {
+            if ((tile += gridDim.x) >= tiles) {
+                add(x);
+                break;
+            }
+            load(tile, y);
+            add(x);
+            if ((tile += gridDim.x) >= tiles) {
+                add(y);
+                break;
+            }
+            load(tile, x);
+            add(y);
+        }
     }
     const double s = block_sum(acc, red);
-    if (tid == 0) sums[blockIdx.x] = s;
+    if (tid == 0) a.sums[blockIdx.x] = s;
 }
 
 // One element: the moments and the parameter.  Every product and sum is rounded by
@@ -153,39 +203,74 @@ struct Step {
     }
 };
 
-// Four elements at p, of which `k` are there; whole vectors where they are aligned.
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, int k, bool vec, float* f) {
-    if (vec && k == 4) {
+// Four elements at p: SOME, `k` of them are there; ALL, one access wherever it starts, and the
+// loads go out without a branch between them; PAST, one access that starts at a multiple of its
+// size and goes past the caches: what the update reads and writes is not met again before the next step, and leaves the gradients of the first
+// pass their place (19.8 M float32 parameters: 108 us a call, 130 without; 71 M
+// of bf16 with masters and 8-bit states 269 and 320; the first pass's own loads: slower so).
+enum How { SOME, ALL, PAST };
+template <typename T> struct Access;
+template <> struct Access<float> {
+    typedef float V __attribute__((ext_vector_type(4)));
+};
+template <> struct Access<bf16_t> {
+    typedef uint32_t V __attribute__((ext_vector_type(2)));
+};
+template <> struct Access<uint8_t> {
+    typedef uint32_t V;
+};
+template <How HOW, typename T>
+__device__ __forceinline__ typename Access<T>::V fetch(const T* p) {
+    typedef typename Access<T>::V V;
+    if constexpr (HOW == PAST) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
+template <How HOW, typename T>
+__device__ __forceinline__ void put(T* p, typename Access<T>::V v) {
+    if constexpr (HOW == PAST) __builtin_nontemporal_store(v, reinterpret_cast<typename Access<T>::V*>(p));
+    else __builtin_memcpy(p, &v, sizeof(v));
+}
+template <How HOW, typename T>
+__device__ __forceinline__ void load4(const T* p, int k, float* f) {
+    if (HOW != SOME || k == 4) {
         Chan<T, 4> v;
-        v.load(p);
+        const typename Access<T>::V x = fetch<HOW>(p);
+        __builtin_memcpy(&v.v, &x, sizeof(x));
         v.get(f);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[j] = j < k ? to_f(p[j]) : 0.f;
     }
 }
-template <typename T>
-__device__ __forceinline__ void store4(T* p, int k, bool vec, const float* f) {
-    if (vec && k == 4) {
-        Chan<T, 4>::store(p, f);
+template <How HOW, typename T>
+__device__ __forceinline__ void store4(T* p, int k, const float* f) {
+    if (HOW != SOME || k == 4) {
+        alignas(16) T v[4];
+        Chan<T, 4>::store(v, f);
+        typename Access<T>::V x;
+        __builtin_memcpy(&x, v, sizeof(x));
+        put<HOW>(p, x);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (j < k) p[j] = out_f<T>(f[j]);
     }
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int k, bool vec) {
-    if (vec && k == 4) return *reinterpret_cast<const uint32_t*>(p);
+template <How HOW>
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int k) {
+    if (HOW != SOME || k == 4) return fetch<HOW>(p);
     uint32_t v = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (j < k) v |= uint32_t(p[j]) << (8 * j);
     return v;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int k, bool vec, uint32_t v) {
-    if (vec && k == 4) {
-        *reinterpret_cast<uint32_t*>(p) = v;
+template <How HOW>
+__device__ __forceinline__ void store_codes(uint8_t* p, int k, uint32_t v) {
+    if (HOW != SOME || k == 4) {
+        put<HOW>(p, v);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -247,88 +332,157 @@ __device__ bool form_step(const AdamArgs& a, Step& st, Control& c, bool report) 
     return go;
 }
 
-__device__ __forceinline__ bool aligned4(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
+// Four elements of a tensor, from element e on: k of them are there.
 template <typename T, bool Q>
-__device__ __forceinline__ void adamw_tile(const janus_adamw_tensor& t, const Step& st, uint32_t key, int64_t at) {
-    const int64_t left = t.size - at;
-    const int len = int(left < kTile ? left : kTile);
-    const float* g = t.g + at;
-    T* p = static_cast<T*>(t.p) + at;
-    float* w = t.master ? t.master + at : nullptr;
-    const bool vg = aligned4(g, 16), vp = aligned4(p, 4 * sizeof(T)), vw = aligned4(w, 16);
-#pragma unroll 2
-    for (int u = 0; u < kTile / 4 / kThreads; ++u) {
-        const int e = (threadIdx.x + u * kThreads) * 4;
-        if ((e & ~255) >= len) break;                    // (256 elements are a wave's: it goes on as a whole)
-        const int k = min(max(len - e, 0), 4);
-        float gf[4], pf[4], m[4], v[4], r[4];
-        load4(g + e, k, vg, gf);
-        if (w) load4(w + e, k, vw, pf);
-        else load4(p + e, k, vp, pf);
+__device__ __forceinline__ bool even(const janus_adamw_tensor& t) {
+    auto at = [](const void* p) { return uint32_t(reinterpret_cast<uintptr_t>(p)); };
+    return ((at(t.p) & (4 * sizeof(T) - 1)) | (at(t.g) & 15u) | (at(t.master) & 15u) | ((at(t.m) | at(t.v)) & (Q ? 3u : 15u))) == 0;
+}
+template <typename T, bool Q>
+struct Four {
+    float g[4], p[4], m[4], v[4];
+    uint32_t mc, vc;
+    float2 scale;
+    int k;
+    template <How HOW>
+    __device__ __forceinline__ void load(const janus_adamw_tensor& t, int64_t e) {
+        k = HOW != SOME ? 4 : int(min(max(t.size - e, int64_t(0)), int64_t(4)));
+        load4<HOW>(t.g + e, k, g);
+        if (t.master) load4<HOW>(t.master + e, k, p);
+        else load4<HOW>(static_cast<const T*>(t.p) + e, k, p);
         if constexpr (Q) {
-            uint8_t *mc = static_cast<uint8_t*>(t.m) + at + e, *vc = static_cast<uint8_t*>(t.v) + at + e;
-            const bool vm = aligned4(t.m, 4), vv = aligned4(t.v, 4);
-            float2* sp = reinterpret_cast<float2*>(t.scale + (at + e) / 256 * 2);
-            const float2 sc = *sp;
-            decode(load_codes(mc, k, vm), sc.x, m);
-            decode(load_codes(vc, k, vv), sc.y, v);
+            mc = load_codes<HOW>(static_cast<const uint8_t*>(t.m) + e, k);
+            vc = load_codes<HOW>(static_cast<const uint8_t*>(t.v) + e, k);
+            scale = *reinterpret_cast<const float2*>(t.scale + e / 256 * 2);
+        } else {
+            load4<HOW>(static_cast<const float*>(t.m) + e, k, m);
+            load4<HOW>(static_cast<const float*>(t.v) + e, k, v);
+        }
+    }
+    template <How HOW>
+    __device__ __forceinline__ void finish(const janus_adamw_tensor& t, int64_t e, const Step& st, uint32_t key) {
+        float r[4];
+        if constexpr (Q) {
+            decode(mc, scale.x, m);
+            decode(vc, scale.y, v);
             uint32_t rm[4], rv[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 v[j] = v[j] * v[j];
-                st.moments(gf[j], m[j], v[j]);
+                st.moments(g[j], m[j], v[j]);
                 r[j] = __fsqrt_rn(v[j]);
-                const uint32_t x = mix(uint32_t(at + e + j) ^ key);
+                const uint32_t x = mix(uint32_t(e + j) ^ key);
                 rm[j] = x & 0xffffu, rv[j] = x >> 16;
             }
-            float sm, sv;
-            const uint32_t cm = encode(m, rm, sm), cv = encode(r, rv, sv);
-            store_codes(mc, k, vm, cm);
-            store_codes(vc, k, vv, cv);
-            if ((threadIdx.x & 63) == 0) *sp = make_float2(sm, sv);
+            float2 s;
+            const uint32_t cm = encode(m, rm, s.x), cv = encode(r, rv, s.y);
+            store_codes<HOW>(static_cast<uint8_t*>(t.m) + e, k, cm);
+            store_codes<HOW>(static_cast<uint8_t*>(t.v) + e, k, cv);
+            if ((threadIdx.x & 63) == 0) *reinterpret_cast<float2*>(t.scale + e / 256 * 2) = s;
         } else {
-            float *mp = static_cast<float*>(t.m) + at + e, *vp_ = static_cast<float*>(t.v) + at + e;
-            const bool vm = aligned4(t.m, 16), vv = aligned4(t.v, 16);
-            load4(mp, k, vm, m);
-            load4(vp_, k, vv, v);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                st.moments(gf[j], m[j], v[j]);
+                st.moments(g[j], m[j], v[j]);
                 r[j] = sqrtf(v[j]);
             }
-            store4(mp, k, vm, m);
-            store4(vp_, k, vv, v);
+            store4<HOW>(static_cast<float*>(t.m) + e, k, m);
+            store4<HOW>(static_cast<float*>(t.v) + e, k, v);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) pf[j] = st.parameter(pf[j], m[j], r[j]);
-        if (w) store4(w + e, k, vw, pf);
-        store4(p + e, k, vp, pf);
+        for (int j = 0; j < 4; ++j) p[j] = st.parameter(p[j], m[j], r[j]);
+        if (t.master) store4<HOW>(t.master + e, k, p);
+        store4<HOW>(static_cast<T*>(t.p) + e, k, p);
     }
+};
+
+// A tile; form() gives the step, and false when nothing may change: after the tile's first loads
+// went out.  PAST: the tile is whole, and so are its accesses.
+template <typename T, bool Q, How HOW, int TILE, typename F>
+__device__ __forceinline__ bool adamw_tile(const janus_adamw_tensor& t, int64_t at, F form) {
+    constexpr int U = TILE / 4 / kThreads, W = U < 2 ? U : 2;
+    Step st{};
+    uint32_t key = 0;
+#pragma unroll 1
+    for (int u = 0; u < U; u += W) {
+        Four<T, Q> x[W];
+        int64_t e[W], end[W];   // end: of the wave's 256 elements
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            e[w] = at + int64_t(threadIdx.x + (u + w) * kThreads) * 4, end[w] = (e[w] & ~int64_t(255)) + 256;
+            if (HOW == PAST) x[w].template load<PAST>(t, e[w]);
+            else if (end[w] <= t.size) x[w].template load<ALL>(t, e[w]);
+            else if (end[w] - 256 < t.size) x[w].template load<SOME>(t, e[w]);
+        }
+        if (u == 0 && !form(st, key)) return false;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (HOW == PAST) x[w].template finish<PAST>(t, e[w], st, key);
+            else if (end[w] <= t.size) x[w].template finish<ALL>(t, e[w], st, key);
+            else if (end[w] - 256 < t.size) x[w].template finish<SOME>(t, e[w], st, key);
+        }
+    }
+    return true;
 }
 
-template <bool Q>
-__global__ __launch_bounds__(kThreads) void adamw_update_kernel(AdamTable t, AdamArgs a, bool report) {
+template <bool Q, int TILE, typename Table>
+__global__ __launch_bounds__(kThreads) void adamw_update_kernel(Table t, AdamArgs a) {
+    __shared__ int64_t lds[kStarts + 1];
+    prepare(t, lds);
     Step st;
     Control c;
-    if (!form_step(a, st, c, report && blockIdx.x == 0)) return;
-    for (int64_t tile = t.tile[t.n] - 1 - blockIdx.x; tile >= 0; tile -= gridDim.x) {
-        const int i = tensor_of(t, tile);
-        const janus_adamw_tensor& x = t.t[i];
-        st.shrink = c.lr * x.decay;
-        const uint32_t key = mix(c.key ^ uint32_t(t.first + i));
-        const int64_t at = (tile - t.tile[i]) * kTile;
-        if (x.dtype == JANUS_BF16) adamw_tile<bf16_t, Q>(x, st, key, at);
-        else adamw_tile<float, Q>(x, st, key, at);
+    bool formed = false, go = false;
+    for (int64_t tile = start(t, lds, t.n) - 1 - blockIdx.x; tile >= 0 || !formed; tile -= gridDim.x) {
+        if (tile < 0) {   // (nothing to do but to say so)
+            form_step(a, st, c, blockIdx.x == 0);
+            return;
+        }
+        const int i = tensor_of(t, lds, tile);
+        const janus_adamw_tensor x = t.t[i];
+        auto form = [&](Step& s, uint32_t& key) {
+            if (!formed) go = form_step(a, st, c, blockIdx.x == 0);
+            formed = true;
+            st.shrink = c.lr * x.decay;
+            key = mix(c.key ^ uint32_t(i));
+            s = st;
+            return go;
+        };
+        const int64_t at = (tile - start(t, lds, i)) * TILE;
+        const bool there = at + TILE <= x.size;
+        const bool done = x.dtype == JANUS_BF16 ? (there && even<bf16_t, Q>(x) ? adamw_tile<bf16_t, Q, PAST, TILE>(x, at, form)
+                                                                      : adamw_tile<bf16_t, Q, SOME, TILE>(x, at, form))
+                                                : (there && even<float, Q>(x) ? adamw_tile<float, Q, PAST, TILE>(x, at, form)
+                                                                     : adamw_tile<float, Q, SOME, TILE>(x, at, form));
+        if (!done) return;
     }
 }
 
-constexpr int chunks(int n) { return (n + kTable - 1) / kTable; }
-size_t adamw_carve(AdamArgs& a, int n, void* ws) {
+size_t adamw_carve(AdamArgs& a, Tensors& t, int n, void* ws) {
     Carver c(ws);
     a.ctl = c.take<Control>(1);
-    a.sums = c.take<double>(size_t(chunks(n)) * kBlocks);
+    a.sums = c.take<double>(kBlocks);
+    t.n = n;
+    if (n > kTable) t.tile = c.take<int64_t>(n + 1), t.t = c.take<janus_adamw_tensor>(n);
     return c.off;
+}
+
+// Calls of up to this many elements are cut in tiles of 1024, for there to be more of them.
+constexpr int64_t kSmallTotal = 1 << 21;
+
+// The two passes, over a table by value or in the workspace
+template <bool Q, typename Table>
+janus_status adamw_run(const Table& t, const AdamArgs& a, bool small, double total, double bytes, hipStream_t st) {
+    const dim3 blocks(a.n_sums), threads(kThreads);
+    {
+        TraceScope trace("adamw_norm", 2.0 * total, 4.0 * total, st);
+        if (small) hipLaunchKernelGGL((adamw_norm_kernel<1024, Table>), blocks, threads, 0, st, t, a);
+        else hipLaunchKernelGGL((adamw_norm_kernel<4096, Table>), blocks, threads, 0, st, t, a);
+        JANUS_LAUNCH_CHECK();
+    }
+    TraceScope trace("adamw_update", 16.0 * total, bytes, st);
+    if (small) hipLaunchKernelGGL((adamw_update_kernel<Q, 1024, Table>), blocks, threads, 0, st, t, a);
+    else hipLaunchKernelGGL((adamw_update_kernel<Q, 4096, Table>), blocks, threads, 0, st, t, a);
+    JANUS_LAUNCH_CHECK();
+    return JANUS_OK;
 }
 
 bool adamw_desc_ok(const janus_adamw_desc* d) {
@@ -359,7 +513,8 @@ using namespace janus;
 extern "C" size_t janus_adamw_workspace_bytes(const janus_adamw_desc* d) {
     if (!adamw_desc_ok(d) || (d->states != JANUS_ADAMW_F32 && d->states != JANUS_ADAMW_8BIT)) return 0;
     AdamArgs a{};
-    return adamw_carve(a, d->n, nullptr);
+    Tensors t;
+    return adamw_carve(a, t, d->n, nullptr);
 }
 
 extern "C" janus_status janus_adamw_update(const janus_adamw_desc* d, const janus_adamw_tensor* tensors, int64_t* step,
@@ -371,7 +526,8 @@ extern "C" janus_status janus_adamw_update(const janus_adamw_desc* d, const janu
     janus_status e = adamw_check(d, tensors);
     if (e != JANUS_OK) return e;
     AdamArgs a{};
-    const size_t need = adamw_carve(a, d->n, ws);
+    Tensors big;
+    const size_t need = adamw_carve(a, big, d->n, ws);
     if (!ws || ws_bytes < need || !aligned(ws, 256)) return JANUS_ERR_WORKSPACE;
     a.b1 = d->beta1, a.b2 = d->beta2;
     a.c1 = float(1.0 - double(d->beta1)), a.c2 = float(1.0 - double(d->beta2));
@@ -379,40 +535,33 @@ extern "C" janus_status janus_adamw_update(const janus_adamw_desc* d, const janu
     a.step = step, a.lr_dev = lr, a.hold = hold, a.stats = stats;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool q = d->states == JANUS_ADAMW_8BIT;
-    auto tiles = [](int64_t size) { return (size + kTile - 1) / kTile; };
-    double* sums = a.sums;
-    for (int c = 0; c < chunks(d->n); ++c) {
-        NormTable t{};
-        const int i0 = c * kTable;
-        t.n = std::min(d->n - i0, kTable);
-        for (int i = 0; i < t.n; ++i) {
-            t.g[i] = tensors[i0 + i].g, t.size[i] = tensors[i0 + i].size;
-            t.tile[i + 1] = t.tile[i] + tiles(t.size[i]);
-        }
-        const int blocks = int(std::max<int64_t>(1, std::min<int64_t>(kBlocks, t.tile[t.n])));
-        TraceScope trace("adamw_norm", 2.0 * kTile * double(t.tile[t.n]), 4.0 * kTile * double(t.tile[t.n]), st);
-        hipLaunchKernelGGL(adamw_norm_kernel, dim3(blocks), dim3(kThreads), 0, st, t, a, sums, c == 0);
-        JANUS_LAUNCH_CHECK();
-        sums += blocks;
-        a.n_sums += blocks;
+    int64_t total = 0;
+    double bytes = 0.0;
+    for (int i = 0; i < d->n; ++i) {
+        const janus_adamw_tensor& x = tensors[i];
+        total += x.size;
+        bytes += double(x.size) * (4 + 2 * double(dtype_size(x.dtype)) + (q ? 4 : 16) + (x.master ? 8 : 0));
     }
-    for (int c = 0; c < chunks(d->n); ++c) {
-        AdamTable t{};
-        const int i0 = c * kTable;
-        t.n = std::min(d->n - i0, kTable), t.first = i0;
-        double bytes = 0.0;
-        for (int i = 0; i < t.n; ++i) {
-            t.t[i] = tensors[i0 + i];
-            t.tile[i + 1] = t.tile[i] + tiles(t.t[i].size);
-            bytes += double(t.t[i].size) * (4 + 2 * double(dtype_size(t.t[i].dtype)) + (q ? 4 : 16) + (t.t[i].master ? 8 : 0));
+    const bool small = total <= kSmallTotal;
+    const int64_t tile = small ? 1024 : 4096;
+    TensorTable t{};
+    int64_t tiles = 0;
+    for (int i = 0; i < d->n; i += kTable) {
+        t.n = std::min(d->n - i, kTable), t.first = i;
+        t.tile[0] = tiles;
+        for (int k = 0; k < t.n; ++k) {
+            t.t[k] = tensors[i + k];
+            t.tile[k + 1] = tiles += (t.t[k].size + tile - 1) / tile;
         }
-        const int blocks = int(std::max<int64_t>(1, std::min<int64_t>(kBlocks, t.tile[t.n])));
-        TraceScope trace("adamw_update", 16.0 * kTile * double(t.tile[t.n]), bytes, st);
-        // (the last launch reports: every other one has read the step's number by then)
-        const bool report = c == chunks(d->n) - 1;
-        if (q) hipLaunchKernelGGL(adamw_update_kernel<true>, dim3(blocks), dim3(kThreads), 0, st, t, a, report);
-        else hipLaunchKernelGGL(adamw_update_kernel<false>, dim3(blocks), dim3(kThreads), 0, st, t, a, report);
-        JANUS_LAUNCH_CHECK();
+        if (d->n > kTable) {
+            TraceScope trace("adamw_table", 0.0, double(sizeof(TensorTable)), st);
+            hipLaunchKernelGGL(adamw_table_kernel, dim3(1), dim3(64), 0, st, t, const_cast<int64_t*>(big.tile),
+                               const_cast<janus_adamw_tensor*>(big.t));
+            JANUS_LAUNCH_CHECK();
+        }
     }
-    return JANUS_OK;
+    a.n_sums = int(std::max<int64_t>(1, std::min<int64_t>(kBlocks, tiles)));
+    if (d->n > kTable) return q ? adamw_run<true>(big, a, small, double(total), bytes, st)
+                                : adamw_run<false>(big, a, small, double(total), bytes, st);
+    return q ? adamw_run<true>(t, a, small, double(total), bytes, st) : adamw_run<false>(t, a, small, double(total), bytes, st);
 }
