@@ -6,11 +6,11 @@
 //   dx = rstd (g - sum g / D - xh sum(g xh) / D) + dh
 //   dgamma = sum dy xh,  dbeta = sum dy   (over rows)
 //
-// A row belongs to a group of 16 or 64 lanes, or to a workgroup, and stays in
-// registers from its mean to its result, so every tensor is read and written
-// once.  In the backward a lane has the same columns in every row it meets and adds
-// up their dgamma and dbeta; workgroups' sums go to the workspace, and a second
-// kernel adds them up in their order.  Everything between loads and stores is
+// A row belongs to a group of 16 to 1024 threads, 8 elements a thread where that
+// suffices, and stays in registers from its mean to its result, so every tensor is
+// read and written once.  In the backward a thread has the same columns in every row it
+// meets and adds up their dgamma and dbeta; workgroups' sums go to the workspace, and a
+// second kernel adds them up in their order.  Everything between loads and stores is
 // float32; the variance is that of the differences from the mean (a mean of squares
 // less the square of the mean loses what a large mean has in common).
 #include <cmath>
@@ -33,7 +33,7 @@ struct NormArgs {
     float* part;           // [gridDim.x][2][D] sums of dgamma and dbeta, or NULL
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;   // of a workgroup, or a row's where that is more
 
 // N sums over the LANES threads of a row (a power of two; above 64 a workgroup's)
 template <int LANES, int N>
@@ -45,17 +45,17 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float* red) {
         for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o, 64);
     if constexpr (LANES > 64) {
         constexpr int WAVES = LANES / 64;
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = threadIdx.x / LANES * WAVES;
         __syncthreads();   // (the sums before have been read)
         if (lane == 0)
 #pragma unroll
-            for (int k = 0; k < N; ++k) red[k * WAVES + wave] = v[k];
+            for (int k = 0; k < N; ++k) red[wave * N + k] = v[k];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             v[k] = 0.f;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) v[k] += red[k * WAVES + w];
+            for (int w = 0; w < WAVES; ++w) v[k] += red[(first + w) * N + k];
         }
     }
 }
@@ -185,9 +185,10 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
 
 // As the forward; a workgroup takes every gridDim.x-th group of rows.  P = 0: dx
 // alone, by two reads of a row.
+constexpr int kBwdThreads = 512;   // (the fewer workgroups, the fewer sums of dgamma and dbeta)
 template <typename T, int VEC, int LANES, int P>
-__global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_bwd_kernel(NormArgs a) {
-    constexpr int THREADS = LANES > kThreads ? LANES : kThreads, ROWS = THREADS / LANES, E = P * VEC;
+__global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void norm_bwd_kernel(NormArgs a) {
+    constexpr int THREADS = LANES > kBwdThreads ? LANES : kBwdThreads, ROWS = THREADS / LANES, E = P * VEC;
     __shared__ float red[2 * THREADS / 64];
     const int tid = threadIdx.x % LANES, at = threadIdx.x / LANES;
     if constexpr (P > 0) {
@@ -251,7 +252,7 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_bwd_
             }
         }
         if (!a.part) return;
-        // the workgroup's groups of lanes, one after another
+        // the workgroup's groups of lanes together
         float* to = a.part + int64_t(blockIdx.x) * 2 * a.D;
         if constexpr (ROWS == 1) {
 #pragma unroll
@@ -262,23 +263,19 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_bwd_
                     if (c < a.D) to[c] = dg[i * VEC + j], to[a.D + c] = db[i * VEC + j];
                 }
         } else {
-            __shared__ float sums[LANES * E];
+            __shared__ float sums[THREADS * E];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                for (int n = 0; n < ROWS; ++n) {
-                    __syncthreads();
-                    if (at == n)
+                __syncthreads();
 #pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const float v = k ? db[e] : dg[e];
-                            float& to_ = sums[e * LANES + tid];
-                            to_ = n ? to_ + v : v;
-                        }
-                }
+                for (int e = 0; e < E; ++e) sums[(at * E + e) * LANES + tid] = k ? db[e] : dg[e];
                 __syncthreads();
                 for (int t = threadIdx.x; t < LANES * E; t += THREADS) {
                     const int e = t / LANES, c = (t % LANES + (e / VEC) * LANES) * VEC + e % VEC;
-                    if (c < a.D) to[k * a.D + c] = sums[t];
+                    float v = 0.f;
+#pragma unroll 8
+                    for (int n = 0; n < ROWS; ++n) v += sums[n * LANES * E + t];
+                    if (c < a.D) to[k * a.D + c] = v;
                 }
             }
         }
@@ -348,24 +345,45 @@ __global__ __launch_bounds__(kThreads) void norm_cols_kernel(NormArgs a) {
     to[a.D + c] = db;
 }
 
-// The workgroups' sums, added up: 64 columns a workgroup, its waves every 16th sum.
+// The workgroups' sums, added up: 64 columns of dgamma or dbeta a workgroup, four of
+// them and every 64th sum a thread.
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* part, int n, int D, float* dgamma, float* dbeta) {
-    __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = int64_t(blockIdx.x) * 64 + lane, width = 2 * int64_t(D);
-    float s = 0.f;
-    if (c < width)
-        for (int k = wave; k < n; k += 16) s += part[k * width + c];
-    red[wave][lane] = s;
-    __syncthreads();
-    if (wave || c >= width) return;
-    s = 0.f;
+    __shared__ float4 red[64][16];
+    const int col = threadIdx.x & 15, from = threadIdx.x >> 4;
+    const int64_t width = 2 * int64_t(D), c = int64_t(blockIdx.x) * 64 + 4 * col;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (D % 4 == 0) {
+        if (c < width) {
+#pragma unroll 4
+            for (int k = from; k < n; k += 64) {
+                const float4 v = *reinterpret_cast<const float4*>(part + k * width + c);
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            }
+        }
+    } else {
+        float f[4] = {};
+        for (int k = from; k < n; k += 64)
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += red[k][lane];
-    if (c < D) {
-        if (dgamma) dgamma[c] = s;
+            for (int j = 0; j < 4; ++j)
+                if (c + j < width) f[j] += part[k * width + c + j];
+        s = make_float4(f[0], f[1], f[2], f[3]);
+    }
+    red[from][col] = s;
+    __syncthreads();
+    // a wave a quarter of the columns, 16 of the 64 sums a lane
+    if (threadIdx.x >= 256) return;
+    const int at = threadIdx.x >> 2;   // the column
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v += reinterpret_cast<const float*>(&red[(threadIdx.x & 3) * 16 + k][at >> 2])[at & 3];
+    v += __shfl_xor(v, 1, 64);
+    v += __shfl_xor(v, 2, 64);
+    const int64_t to = int64_t(blockIdx.x) * 64 + at;
+    if ((threadIdx.x & 3) || to >= width) return;
+    if (to < D) {
+        if (dgamma) dgamma[to] = v;
     } else if (dbeta) {
-        dbeta[c - D] = s;
+        dbeta[to - D] = v;
     }
 }
 __global__ __launch_bounds__(kThreads) void norm_zero_kernel(float* dgamma, float* dbeta, int D) {
@@ -375,10 +393,10 @@ __global__ __launch_bounds__(kThreads) void norm_zero_kernel(float* dgamma, floa
     if (dbeta) dbeta[c] = 0.f;
 }
 
-// A backward of at most this many workgroups: four of 256 threads on each CU.
-constexpr int kNormBlocks = 1024;
-// Rows of more elements than this never fit the registers (32 elements a lane).
-constexpr int kMostHeld = 1024 * 32;
+// A backward of at most this many workgroups: two of 512 threads on each CU.
+constexpr int kNormBlocks = 512;
+// Rows of more elements than this never fit the registers (16 elements a thread).
+constexpr int kMostHeld = 1024 * 16;
 
 // Workgroups of norm_cols_kernel over the rows
 int cols_parts(int32_t rows, int32_t D) {
@@ -447,20 +465,31 @@ bool fwd_lanes(const NormArgs& a, int64_t n, hipStream_t st) {
     if constexpr (sizeof...(MORE) > 0) return fwd_lanes<T, VEC, LANES, MORE...>(a, n, st);
     else return false;
 }
+// From this many rows on a forward gives a bf16 row of up to 2048 elements a wave, which waits for no
+// other one: 65536 rows of 2048 with a residual 204 us, in workgroups 216 (float32 rows hold twice the
+// registers: 25600 of 2048 81 and 73 us).  Fewer rows leave the chip idle that way: 20 rows of 1300
+// take 3.9 us in workgroups of 256, and 5.1.
+constexpr int kWaveRows = 4096;
 template <typename T, int VEC>
 void fwd_vec(const NormArgs& a, hipStream_t st) {
     const int64_t n = (int64_t(a.D) + VEC - 1) / VEC;   // accesses a row
-    constexpr int MOST = VEC < 8 ? 8 : 4;   // at most 32 elements a lane
-    if (fwd_lanes<T, VEC, 16, 1, 2>(a, n, st) || fwd_lanes<T, VEC, 64, 1, 2, 4, MOST>(a, n, st) ||
-        fwd_lanes<T, VEC, 256, 4, MOST>(a, n, st) || fwd_lanes<T, VEC, 1024, 4, MOST>(a, n, st))
+    constexpr int P = 8 / VEC;
+    if (fwd_lanes<T, VEC, 16, P>(a, n, st)) return;
+    if constexpr (sizeof(T) == 2)
+        if (a.rows >= kWaveRows && fwd_lanes<T, VEC, 64, P, 2 * P, 4 * P>(a, n, st)) return;
+    if (fwd_lanes<T, VEC, 64, P>(a, n, st) || fwd_lanes<T, VEC, 128, P>(a, n, st) ||
+        fwd_lanes<T, VEC, 256, P>(a, n, st) || fwd_lanes<T, VEC, 512, P>(a, n, st) ||
+        fwd_lanes<T, VEC, 1024, P, 2 * P>(a, n, st))
         return;
     fwd_launch<T, VEC, 1024, 0>(a, st);
 }
 
 template <typename T, int VEC, int LANES, int P>
 int bwd_launch(const NormArgs& a, hipStream_t st) {
-    constexpr int THREADS = LANES > kThreads ? LANES : kThreads, ROWS = THREADS / LANES;
-    const int blocks = int(std::min<int64_t>((int64_t(a.rows) + ROWS - 1) / ROWS, kNormBlocks));
+    constexpr int THREADS = LANES > kBwdThreads ? LANES : kBwdThreads, ROWS = THREADS / LANES;
+    // (a workgroup's sums cost as much as three or four rows)
+    const int64_t groups = (int64_t(a.rows) + ROWS - 1) / ROWS;
+    const int blocks = int(std::min<int64_t>(groups, std::min<int64_t>(std::max<int64_t>(64, groups / 4), kNormBlocks)));
     hipLaunchKernelGGL((norm_bwd_kernel<T, VEC, LANES, P>), dim3(blocks), dim3(THREADS), 0, st, a);
     return blocks;
 }
@@ -475,11 +504,15 @@ template <typename T, int VEC>
 int bwd_vec(NormArgs a, hipStream_t st) {
     const int64_t n = (int64_t(a.D) + VEC - 1) / VEC;
     int k;
-    if ((k = bwd_lanes<T, VEC, 16, 1, 2>(a, n, st))) return k;
-    constexpr int MOST = VEC < 8 ? 8 : 4;   // at most 32 elements a lane
-    if ((k = bwd_lanes<T, VEC, 64, 1, 2, 4, MOST>(a, n, st))) return k;
-    if ((k = bwd_lanes<T, VEC, 256, 4, MOST>(a, n, st))) return k;
-    if ((k = bwd_lanes<T, VEC, 1024, 4, MOST>(a, n, st))) return k;
+    constexpr int P = 8 / VEC;
+    if ((k = bwd_lanes<T, VEC, 16, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, 64, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, 128, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, 256, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, 512, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, 1024, P>(a, n, st))) return k;
+    if constexpr (sizeof(T) == 2)   // (float32: 404 registers spilled)
+        if ((k = bwd_lanes<T, VEC, 1024, 2 * P>(a, n, st))) return k;
     if (a.dx) {   // (a launch holds fewer than 2^32 threads)
         constexpr int64_t kMost = (1 << 30) / 1024;
         const int64_t rows = a.rows, es = sizeof(T);
