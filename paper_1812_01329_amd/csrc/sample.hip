@@ -182,9 +182,9 @@ struct Run {
 };
 
 // Pieces of 16 bytes of a row that LDS holds beside the rest (29 of a CU's 160 KB): in a
-// workgroup of 1024 threads, and in one of 256 (one more where the row starts inside one).
-constexpr int kHeld = 8192, kHeldSmall = 512;
-template <int THREADS> constexpr int kSlots = THREADS == 256 ? 2 : 8;   // a thread's, in a row of whole pieces
+// workgroup of 1024 threads, in one of 256 and in one of 512 (one more where the row starts inside one).
+constexpr int kHeld = 8192, kHeldSmall = 512, kHeldMiddle = 2048;
+template <int THREADS> constexpr int kSlots = THREADS == 256 ? 2 : THREADS == 512 ? 4 : 8;   // a thread's, in a row of whole pieces
 constexpr size_t held_bytes(int64_t np) { return size_t(np + 8) * 16; }  // (the last thread's pieces are turned as well)
 
 // HELD: the row is in LDS, a thread has `slots` pieces one after another; else a wave
@@ -249,10 +249,10 @@ struct Sampler {
             if (k < slots) v[k] = from[min(int(threadIdx.x) + k * THREADS, np - 1)];
     }
     // The first pass, which brings the row to LDS (any thread meets any element): the
-    // largest of what the thread met, and whether any was NaN.
-    __device__ __forceinline__ void largest(const uint4 (&v)[kSlots<THREADS>], float& own, bool& nan) const {
+    // largest of what the thread met, and whether any was NaN, and any -inf (or may be).
+    __device__ __forceinline__ void largest(const uint4 (&v)[kSlots<THREADS>], float& own, bool& nan, bool& holes) const {
         typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
-        own = -INFINITY, nan = false;
+        own = -INFINITY, nan = false, holes = true;
         ushort2_t bits = {0, 0};   // (the largest of bf16 values' bits without the sign)
         auto meet = [&](const Piece<T>& x) {
 #pragma unroll
@@ -292,7 +292,7 @@ struct Sampler {
                 if (piece(i, p, x)) meet(x);
             }
         }
-        if constexpr (sizeof(T) == 2) nan = max(bits.x, bits.y) > 0x7f80;
+        if constexpr (sizeof(T) == 2) nan = max(bits.x, bits.y) > 0x7f80, holes = max(bits.x, bits.y) == 0x7f80;
     }
 
     // sum over the workgroup of a number a wave has (in all its lanes), and over the waves before
@@ -437,14 +437,14 @@ struct Sampler {
     }
 
     // Shortens the run to its first `need` elements, or (MASS) to the shortest one with the
-    // share p of its weight.  low: the smallest live logit.
+    // share p of its weight.  low: the smallest live logit.  total: with weights in
+    // bins from gather(), the weight of all (else 0).
     template <bool MASS>
-    __device__ __forceinline__ void shorten(Run& run, u64 need, float p, float low) {
+    __device__ __forceinline__ void shorten(Run& run, u64 need, float p, float low, u64 total) {
         constexpr int PER = kBins / THREADS;
         const int tid = threadIdx.x;
         uint32_t lo = 0, hi = 0xffffffffu;   // keys among which the run's end is
-        // (weights: bins of 1/32 of a power of two, the last one for all below 2^-32)
-        const float scale = MASS ? 32.f * float(weight.c) : m > low ? float(kBins) / (m - low) : 0.f;
+        const float scale = MASS ? bin_scale() : m > low ? float(kBins) / (m - low) : 0.f;
         for (int level = 0;; ++level) {
             const int sft = level ? max(0, 32 - __clz(int(hi - lo)) - 10) : 0;
             auto member = [&](float v, uint32_t k, int j) { return v > -INFINITY && k >= lo && k <= hi && run.has(k, j); };
@@ -453,25 +453,33 @@ struct Sampler {
                 const float b = (m - v) * scale;
                 return b < float(kBins - 1) ? int(b) : kBins - 1;   // (0 * inf of far values: the last)
             };
+            const bool binned = MASS && level == 0 && total;
+            if (!binned) {
+                __syncthreads();
 #pragma unroll
-            for (int t = 0; t < PER; ++t) {
-                sh.count[tid + t * THREADS] = 0;
-                if (MASS) sh.mass[tid + t * THREADS] = 0;
+                for (int t = 0; t < PER; ++t) {
+                    sh.count[tid + t * THREADS] = 0;
+                    if (MASS) sh.mass[tid + t * THREADS] = 0;
+                }
+                __syncthreads();
+                each([&](float v, int j) {
+                    const uint32_t k = key_of(v);
+                    if (!member(v, k, j)) return;
+                    const int b = bin(v, k);
+                    atomicAdd(&sh.count[b], 1u);
+                    if (MASS) atomicAdd(&sh.mass[b], weight(v));
+                });
             }
-            __syncthreads();
-            each([&](float v, int j) {
-                const uint32_t k = key_of(v);
-                if (!member(v, k, j)) return;
-                const int b = bin(v, k);
-                atomicAdd(&sh.count[b], 1u);
-                if (MASS) atomicAdd(&sh.mass[b], weight(v));
-            });
             __syncthreads();
             // a thread has PER bins; `own` what they hold
             u64 own = 0, all;
 #pragma unroll
             for (int t = 0; t < PER; ++t) own += MASS ? sh.mass[tid * PER + t] : u64(sh.count[tid * PER + t]);
             u64 before = threads_before(own, all);
+            if (binned) {   // (the last bin's weight is what the others leave)
+                if (tid == THREADS - 1) sh.mass[kBins - 1] += total - all;
+                all = total;
+            }
             if (MASS && level == 0) need = share(p, all);
 #pragma unroll
             for (int t = 0; t < PER; ++t) {
@@ -484,17 +492,42 @@ struct Sampler {
             }
             __syncthreads();
             const int b = sh.bin;
-            const uint32_t n = sh.count[b];
             need -= sh.before;
             auto inside = [&](float v, uint32_t k, int j) { return member(v, k, j) && bin(v, k) == b; };
-            if (n <= uint32_t(kPairs)) {
+            __syncthreads();   // (all have read)
+            // list the bin's elements, as far as there is room
+            uint32_t n = binned ? 0 : sh.count[b];
+            if (binned || n <= uint32_t(kPairs)) {
                 __syncthreads();   // (sh.count is read before it is cleared)
                 if (tid < kPairs) sh.count[tid] = 0, sh.mass[tid] = 0;
-                each([&](float v, int j) {
-                    const uint32_t k = key_of(v);
-                    if (inside(v, k, j)) sh.list[atomicAdd(&sh.n, 1u)] = Entry{place_of(k, j), MASS ? weight(v) : 1};
-                });
+                auto put = [&](float v, uint32_t k, int j) {
+                    const uint32_t at = atomicAdd(&sh.n, 1u);
+                    if (at < uint32_t(kPairs)) sh.list[at] = Entry{place_of(k, j), MASS ? weight(v) : 1};
+                };
+                if (binned && few()) {
+                    u64 marks = 0;
+#pragma unroll 1
+                    for (int i = 0; i < slots; ++i) {
+                        int at;
+                        Piece<T> v;
+                        if (!piece(i, at, v)) break;
+                        marks |= u64(mark(v, [&](float x) { return x > -INFINITY && bin(x, 0) == b; })) << (i * VEC);
+                    }
+                    for (; marks; marks &= marks - 1) {
+                        int j;
+                        const float v = marked(__ffsll(marks) - 1, j);
+                        put(v, key_of(v), j);
+                    }
+                } else {
+                    each([&](float v, int j) {
+                        const uint32_t k = key_of(v);
+                        if (inside(v, k, j)) put(v, k, j);
+                    });
+                }
                 __syncthreads();
+                n = sh.n;
+            }
+            if (n <= uint32_t(kPairs)) {
                 pairs<false>(int(n));
                 __syncthreads();
                 if (tid < int(n)) {
@@ -535,11 +568,16 @@ struct Sampler {
     }
 
     // One pass over the row for what is wanted of it: the sum of exp(x - m); the sum of the
-    // weights of all and the number of live ones; which elements are at least `least`
-    // (a bit each, the first 64 of the thread's).
-    __device__ __forceinline__ void gather(bool want_e, bool want_w, float least, float& e, u64& mine, uint32_t& live,
-                                           u64& marks) const {
-        e = 0.f, mine = 0, live = 0, marks = 0;
+    // weights of all, the number of live ones, and the weights in bins (below); which elements
+    // are at least `least` (a bit each, the first 64 of the thread's).
+    struct Gathered {
+        float e = 0.f;
+        u64 mine = 0, marks = 0;
+        uint32_t live = 0;
+    };
+    __device__ __forceinline__ Gathered gather(bool want_e, bool want_w, bool want_live, bool want_bins, float least) const {
+        Gathered g;
+        const float scale = bin_scale();
 #pragma unroll 1
         for (int i = 0; i < slots; ++i) {
             int p;
@@ -547,27 +585,52 @@ struct Sampler {
             if (!piece(i, p, v)) break;
             if (want_e) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) e += __builtin_amdgcn_exp2f((v.get(j) - m) * kLog2e);
+                for (int j = 0; j < VEC; ++j) g.e += __builtin_amdgcn_exp2f((v.get(j) - m) * kLog2e);
             }
-            if (want_w) {
+            if (want_bins) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) mine += weight.raw(v.get(j)), live += v.get(j) > -INFINITY;
-                mine -= VEC * Weight::kOne;
-            }
-            if (least > -INFINITY) {
-                uint32_t bits = 0;
+                for (int j = 0; j < VEC; ++j) {
+                    const u64 w = weight(v.get(j));
+                    const float b = (m - v.get(j)) * scale;
+                    g.mine += w;
+                    if (b < float(kBins - 1)) atomicAdd(&sh.mass[int(b)], w);
+                }
+            } else if (want_w) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) bits |= v.get(j) >= least ? 1u << j : 0u;
-                marks |= u64(bits) << (i * VEC & 63);
+                for (int j = 0; j < VEC; ++j) g.mine += weight.raw(v.get(j));
+                g.mine -= VEC * Weight::kOne;
             }
+            if (want_live) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) g.live += v.get(j) > -INFINITY;
+            }
+            if (least > -INFINITY) g.marks |= u64(mark(v, [&](float x) { return x >= least; })) << (i * VEC & 63);
         }
+        return g;
     }
+    // a bit for each of a piece's elements
+    template <typename F>
+    __device__ __forceinline__ uint32_t mark(const Piece<T>& v, F f) const {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) bits |= f(v.get(j)) ? 1u << j : 0u;
+        return bits;
+    }
+    // the thread's element of a bit, and its index
+    __device__ __forceinline__ float marked(int bit, int& index) const {
+        const int i = bit / VEC, j = bit % VEC, p = HELD ? first + i : first + i * 64;
+        index = p * VEC + j - row.lo;
+        if constexpr (HELD) return to_f(reinterpret_cast<const T*>(&held_row[held_at(first, turn, i)])[j]);
+        else return to_f(row.base[p * VEC + j]);
+    }
+    __device__ __forceinline__ bool few() const { return slots * VEC <= 64; }   // (a bit is one element)
+    // Bins of weights: 1/32 of a power of two each, the last one all below 2^-32
+    __device__ __forceinline__ float bin_scale() const { return 32.f * float(weight.c); }
     // Lists the marked elements (their number in sh.n, which may be more than there is room for)
     __device__ __forceinline__ void list(float least, u64 marks) const {
         const int lane = threadIdx.x & 63;
-        const bool few = slots * VEC <= 64;   // (else a bit may stand for two elements: all are looked at again)
         uint32_t c = uint32_t(__popcll(marks));
-        if (!few) {
+        if (!few()) {   // (a bit may stand for two elements: all are looked at again)
             c = 0;
             if (marks) each([&](float v, int) { c += v >= least; });
         }
@@ -580,19 +643,16 @@ struct Sampler {
                 if (at < uint32_t(THREADS)) sh.list[at].at = place_of(key_of(v), j);
                 ++at;
             };
-            if (!few) {
+            if (!few()) {
                 if (c)
                     each([&](float v, int j) {
                         if (v >= least) put(v, j);
                     });
             } else {
                 for (; marks; marks &= marks - 1) {
-                    const int bit = __ffsll(marks) - 1, i = bit / VEC, j = bit % VEC;
-                    const int p = HELD ? first + i : first + i * 64, e = p * VEC + j;
-                    float v;
-                    if constexpr (HELD) v = to_f(reinterpret_cast<const T*>(&held_row[held_at(first, turn, i)])[j]);
-                    else v = to_f(row.base[e]);
-                    put(v, e - row.lo);
+                    int j;
+                    const float v = marked(__ffsll(marks) - 1, j);
+                    put(v, j);
                 }
             }
         }
@@ -644,23 +704,24 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
 
     // the largest logit of the thread and of the row, the smallest of the threads' largest
     float own;
-    bool nan;
-    s.largest(pieces, own, nan);
+    bool nan, holes;
+    s.largest(pieces, own, nan, holes);
     if (more) {   // the next row is on its way while this one is worked on
         const Sampler<T, THREADS, HELD> after(static_cast<const T*>(a.logits) + (r + int64_t(gridDim.x)) * a.ld, a.V, sh);
         if (after.pieces_whole()) after.fetch(pieces);
     }
     float m = wave_max(own), low = wave_max(own > -INFINITY ? -own : -INFINITY);
-    nan = __ballot(nan) != 0;
-    if (lane == 0) sh.f[0][wave] = m, sh.f[1][wave] = low, sh.f[2][wave] = nan ? 1.f : 0.f;
-    if (tid < kPairs) sh.count[tid] = 0, sh.mass[tid] = 0;
+    nan = __ballot(nan) != 0, holes = __ballot(holes) != 0;
+    if (lane == 0) sh.f[0][wave] = m, sh.f[1][wave] = low, sh.f[2][wave] = nan ? 2.f : holes ? 1.f : 0.f;
+    for (int t = tid; t < kBins; t += THREADS) sh.count[t] = 0, sh.mass[t] = 0;
     if (tid == 0) sh.n = 0, sh.kept = 0, sh.live = 0, sh.total = 0, sh.kept_total = 0;
     const bool greedy = temp == 0.f, some = minp > 0.f && temp < INFINITY && !greedy, part = p < 1.f && !greedy;
     // (a border of log(min_p): long code, one wave's)
     if (some && wave == WAVES - 1) sh.depth = double(temp) * log_of(double(fminf(minp, 1.f)));
     __syncthreads();
     m = wave_max(lane < WAVES ? sh.f[0][lane] : -INFINITY), low = -wave_max(lane < WAVES ? sh.f[1][lane] : -INFINITY);
-    nan = wave_max(lane < WAVES ? sh.f[2][lane] : 0.f) > 0.f;
+    const float found = wave_max(lane < WAVES ? sh.f[2][lane] : 0.f);
+    nan = found == 2.f, holes = found == 1.f;
     if (nan || m == INFINITY || !(temp >= 0.f) || p != p || minp != minp || u != u) {
         if (tid == 0) answer(-1, NAN, NAN, 0);
         return;
@@ -678,24 +739,24 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
     const float least = greedy ? m : k > 0 ? (k <= THREADS ? s.reached_by(uint32_t(k), own, low) : -INFINITY) : border;
     const bool sum_all = !greedy && k <= 0 && (part || !some);   // the weight of all is wanted
     const bool exps = a.logp && !(sum_all && temp == 1.f);
-    float e;
-    u64 mine, marks;
-    uint32_t live;
-    s.gather(exps, sum_all, least, e, mine, live, marks);
+    const bool bins = sum_all && part && !some;
+    const auto g = s.gather(exps, sum_all, sum_all && a.kept && holes, bins, least);
+    u64 mine = g.mine;
+    uint32_t live = holes ? g.live : uint32_t(a.V);
     // sums of all, and of the threads before
     u64 all = 0, before = 0;
     if (sum_all) {
         const u64 up = up_to(mine);
-        if (a.kept) {
+        if (a.kept && holes) {
             const uint32_t c = last_lane(up_to(live));
             if (lane == 0 && c) atomicAdd(&sh.live, c);
         }
         all = s.over_waves(last_lane(up), before);
         before += up - mine;
-        live = sh.live;
+        if (holes) live = sh.live;
     }
     float lse = 0.f;   // the (binary) logarithm of the sum of exp(x - m)
-    if (exps) lse = __builtin_amdgcn_logf(s.over_waves_sum(e));
+    if (exps) lse = __builtin_amdgcn_logf(s.over_waves_sum(g.e));
     else if (a.logp) lse = __builtin_amdgcn_logf(ldexpf(float(all), -a.bits));
     auto logp_of = [&](float x) { return fmaf(-lse, kLn2, x - m); };
     const float chance = fminf(fmaxf(u, 0.f), 1.f);
@@ -705,7 +766,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
     };
 
     if (least > -INFINITY) {
-        s.list(least, marks);
+        s.list(least, g.marks);
         const int n = int(sh.n);
         if (greedy && n <= kPairs) {   // the first of the largest
             if (tid >= 64) return;
@@ -794,20 +855,37 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
         __syncthreads();
         bottom = -wave_max(lane < WAVES ? sh.f[0][lane] : -INFINITY);
         __syncthreads();
-        if (u64(k) < n) s.template shorten<false>(run, u64(k), 0.f, bottom);
+        if (u64(k) < n) s.template shorten<false>(run, u64(k), 0.f, bottom, 0);
     }
-    if (part) s.template shorten<true>(run, 0, p, 0.f);
+    if (part) s.template shorten<true>(run, 0, p, 0.f, bins ? all : 0);
     if (some && key_of(border) > run.key) run.key = key_of(border), run.last = 0x7fffffff;
 
     auto kept = [&](float x, int j) { return x > -INFINITY && run.has(key_of(x), j); };
     if (!sum_all || part) {   // (else added up already)
         mine = 0, live = 0;
-        s.each([&](float x, int j) {
-            const u64 w = s.weight(x);
-            const bool in = kept(x, j);
-            mine += in ? w : 0;
-            live += in;
-        });
+        if (s.few()) {   // a fifth of the row or so: its weights alone
+            u64 marks = 0;
+#pragma unroll 1
+            for (int i = 0; i < s.slots; ++i) {
+                int p;
+                Piece<T> v;
+                if (!s.piece(i, p, v)) break;
+                int j = p * Sampler<T, THREADS, HELD>::VEC - s.row.lo;
+                marks |= u64(s.mark(v, [&](float x) { return kept(x, j++); })) << (i * Sampler<T, THREADS, HELD>::VEC);
+            }
+            live = uint32_t(__popcll(marks));
+            for (; marks; marks &= marks - 1) {
+                int j;
+                mine += s.weight(s.marked(__ffsll(marks) - 1, j));
+            }
+        } else {
+            s.each([&](float x, int j) {
+                const u64 w = s.weight(x);
+                const bool in = kept(x, j);
+                mine += in ? w : 0;
+                live += in;
+            });
+        }
         const u64 up = up_to(mine);
         all = s.over_waves(last_lane(up), before);
         before += up - mine;
@@ -820,7 +898,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
 
 // A workgroup takes every gridDim.x-th row.
 template <typename T, int THREADS, bool HELD>
-__global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a) {
     __shared__ Shared<THREADS> sh;
     uint4 pieces[kSlots<THREADS>];   // the next row's
     for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -873,6 +951,7 @@ template <typename T>
 janus_status sample_dispatch(const SampleArgs& a, hipStream_t st) {
     const int64_t full = (int64_t(a.V) * sizeof(T) + 15) / 16, np = full + 1;   // (a row may start inside a piece)
     if (full <= kHeldSmall) return sample_launch<T, 256, true>(a, np, st);
+    if (full <= kHeldMiddle) return sample_launch<T, 512, true>(a, np, st);
     if (full <= kHeld) return sample_launch<T, 1024, true>(a, np, st);
     return sample_launch<T, 1024, false>(a, np, st);
 }

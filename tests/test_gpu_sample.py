@@ -198,3 +198,45 @@ def test_rows_more_than_2_to_32_elements_apart():
     J.janus_sample(J.SampleDesc(3, V, J.BF16, ld, 1.0, 0, 0.9, 0.0), x, u, tok)
     J.janus_sample(J.SampleDesc(3, V, J.BF16, 0, 1.0, 0, 0.9, 0.0), x.contiguous(), u, want)
     assert torch.equal(tok, want)
+
+
+@pytest.mark.parametrize("dtype,V,shift", [("bf16", 4096, 0), ("bf16", 4097, 0), ("bf16", 16384, 0), ("bf16", 16384, 3), ("bf16", 65536, 0),
+                                           ("bf16", 65536, 5), ("bf16", 65544, 0), ("f32", 2048, 1), ("f32", 8192, 0),
+                                           ("f32", 32768, 2), ("f32", 32772, 0), ("f32", 100000, 0)])
+def test_every_way_to_the_token(dtype, V, shift):
+    """Around the sizes at which a row goes to more threads, or no longer to LDS: lists of a few
+    entries, of hundreds, past what a workgroup lists; bins alone; peaked rows beside flat ones."""
+    print(f"[sample ways] {dtype} {V} {shift}", flush=True)
+    rng = np.random.default_rng(V)
+    settings = [dict(), dict(k=2), dict(k=130), dict(k=500), dict(k=900), dict(k=3000, p=0.9), dict(p=0.97, T=1.5), dict(p=0.4),
+                dict(minp=0.3), dict(minp=0.01, T=1.5), dict(minp=1e-4, T=2.0), dict(minp=0.02, p=0.6), dict(T=0.0), dict(T=1e-3, p=0.99)]
+    flat = rng.normal(size=(len(settings), V)) * 2.5
+    peaked = rng.normal(size=(len(settings), V)) * 1.5
+    peaked[:, rng.integers(0, V, 8)] += 15.0
+    x = np.concatenate([flat, peaked]).astype(np.float32)
+    x = bf16(x) if dtype == "bf16" else x
+    s = {n: [c.get(n, v) for c in settings] * 2 for n, v in dict(T=1.0, k=0, p=1.0, minp=0.0).items()}
+    u = rng.random(len(x)).astype(np.float32)
+    check(x, u, run(x, u, dtype, shift=shift, **s), **s)
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 301), ("bf16", 5000), ("bf16", 20008), ("bf16", 20001), ("f32", 40000)])
+def test_more_rows_than_workgroups(dtype, V):
+    """A workgroup takes several rows one after another: each is what it is alone (logp, a
+    float32 sum whose order follows the row's start in memory, within its tolerance)."""
+    rng = np.random.default_rng(V)
+    R = 1100
+    x = (rng.normal(size=(R, V)) * 2).astype(np.float32)
+    x[::7, 1] = np.nan
+    x[::11] = -np.inf
+    s = dict(T=[1.0, 0.0, 0.8, 1.3] * 275, k=[0, 0, 40, 0, 400] * 220, p=[1.0, 0.9, 1.0, 0.8] * 275, minp=[0.0, 0.0, 0.05, 0.0] * 275)
+    u = rng.random(R).astype(np.float32)
+    got = run(x, u, dtype, **s)
+    for r0 in range(0, R, 100):
+        part = {n: v[r0:r0 + 100] for n, v in s.items()}
+        alone = run(x[r0:r0 + 100], u[r0:r0 + 100], dtype, **part)
+        for i, (a, b) in enumerate(zip(got, alone)):
+            np.testing.assert_allclose(a[r0:r0 + 100], b, rtol=0, atol=2e-5 if i == 1 else 0, equal_nan=True)
+    pick = list(range(0, R, 97))
+    part = {n: [v[i] for i in pick] for n, v in s.items()}
+    check(bf16(x[pick]) if dtype == "bf16" else x[pick], u[pick], [g[pick] for g in got], **part)
