@@ -370,7 +370,7 @@ struct Four {
             for (int j = 0; j < 4; ++j) {
                 v[j] = v[j] * v[j];
                 st.moments(g[j], m[j], v[j]);
-                r[j] = __fsqrt_rn(v[j]);
+                r[j] = sqrtf(v[j]);   // (rounded correctly, as the codes' definition has it; __fsqrt_rn is off by one bit at times)
                 const uint32_t x = mix(uint32_t(e + j) ^ key);
                 rm[j] = x & 0xffffu, rv[j] = x >> 16;
             }

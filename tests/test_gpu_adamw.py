@@ -272,3 +272,27 @@ def test_training_steps_end_in_it(kind, bits, masters):
     up.apply()
     # (the gradients are those of the second step; it has to land on the same bits)
     assert all(torch.equal(p, q) for p, q in zip(up.params, want)) and int(up.step) == 2
+
+
+def test_roots_are_rounded_correctly():
+    """With beta2 0 and no states sqrt(v) is |g| itself: gradients that lie, by the element's
+    random bits, on the border between two codes and one bit below it come out as
+    defined, which a root that is off by its last bit would not."""
+    import torch
+    from paper_1812_01329_amd import janus as J
+    n = 256 * 256
+    rng = np.random.default_rng(12)
+    rnd = oracle.random16(77, 1, 0, n)[1].astype(np.int64)
+    low = ((1 << 20) - (rnd << 4)) % (1 << 20) - np.arange(n) % 2 * (rnd > 0)
+    bits = (rng.integers(121, 134, n) << 23) + (rng.integers(0, 8, n) << 20) + low
+    g = bits.astype(np.uint32).view(F)
+    p, m, v = (torch.zeros(n, dtype=t, device="cuda") for t in (torch.float32, torch.uint8, torch.uint8))
+    scale = torch.zeros(n // 256, 2, device="cuda")
+    d = J.AdamWDesc(1, J.ADAMW_8BIT, 0.1, 0.9, 0.0, 1e-8, 0.0, 77)
+    ws = torch.empty(J.janus_adamw_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    grad = torch.from_numpy(g.copy()).cuda()
+    J.janus_adamw_update(d, J.adamw_tensors([p], [grad], [m], [v], [scale]), step, ws=ws)
+    code, s = oracle.encode(np.sqrt(g.astype(np.float64) ** 2).astype(F), rnd)
+    np.testing.assert_array_equal(scale[:, 1].cpu().numpy(), s)
+    np.testing.assert_array_equal(v.cpu().numpy(), code)
