@@ -22,7 +22,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "seq.hpp"
+#include "rows.hpp"
 
 namespace janus {
 namespace {
@@ -199,7 +199,7 @@ struct Step {
         v = v * b2 + (g * g) * c2;
     }
     __device__ __forceinline__ float parameter(float p, float m, float r) const {
-        return p - p * shrink - rate * m / (r * root + eps);
+        return p - p * shrink - rate * m * __builtin_amdgcn_rcpf(r * root + eps);   // (off by an ulp of the step)
     }
 };
 
@@ -278,6 +278,17 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int k, uint32_t v) {
     }
 }
 
+// sqrt(v), rounded correctly, as the codes' definition has it: the machine's root is off by its last
+// bit at times; of it and its neighbours the one that v lies next to
+__device__ __forceinline__ float root_of(float v) {
+    if (!(v >= 0x1p-64f && v < INFINITY)) return sqrtf(v);   // (the products below would leave float32)
+    const float s = __builtin_amdgcn_sqrtf(v);
+    const float down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
+    // the borders are the squares of the means: (s - ulp / 2)^2 = s down + ulp^2 / 4
+    if (fmaf(-down, s, v) <= 0.f) return down;
+    return fmaf(-up, s, v) > 0.f ? up : s;
+}
+
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void decode(uint32_t codes, float scale, float* f) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(codes), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(codes), true);
@@ -294,8 +305,7 @@ __device__ __forceinline__ uint32_t encode(const float* f, const uint32_t* rnd, 
         a[j] = fminf(fabsf(f[j]), kLargest);
         top = fmaxf(top, a[j]);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    top = wave_max(top);
     // (the exponent goes up by one where the mantissa is past 1.75)
     const uint32_t E = max((__float_as_uint(top) + 0x1FFFFFu) >> 23, 9u);
     scale = __uint_as_float((E - 8u) << 23);
@@ -370,7 +380,7 @@ struct Four {
             for (int j = 0; j < 4; ++j) {
                 v[j] = v[j] * v[j];
                 st.moments(g[j], m[j], v[j]);
-                r[j] = sqrtf(v[j]);   // (rounded correctly, as the codes' definition has it; __fsqrt_rn is off by one bit at times)
+                r[j] = root_of(v[j]);
                 const uint32_t x = mix(uint32_t(e + j) ^ key);
                 rm[j] = x & 0xffffu, rv[j] = x >> 16;
             }
@@ -383,7 +393,7 @@ struct Four {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 st.moments(g[j], m[j], v[j]);
-                r[j] = sqrtf(v[j]);
+                r[j] = __builtin_amdgcn_sqrtf(v[j]);
             }
             store4<HOW>(static_cast<float*>(t.m) + e, k, m);
             store4<HOW>(static_cast<float*>(t.v) + e, k, v);

@@ -1,5 +1,5 @@
-// What the kernels that work on whole rows share: sums over a wave, and rows read
-// in pieces of 16 bytes wherever they start.
+// What the kernels that work on whole rows or blocks share: sums, scans and maxima over
+// a wave, and rows read in pieces of 16 bytes wherever they start.
 #pragma once
 
 #include "seq.hpp"
@@ -20,6 +20,45 @@ __device__ __forceinline__ double wsum(double v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
+}
+
+typedef unsigned long long u64;
+
+// ---- sums, scans and maxima over a wave, by moves between neighbouring lanes and rows of 16
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t old, uint32_t v) {
+    return uint32_t(__builtin_amdgcn_update_dpp(int(old), int(v), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 old, u64 v) {
+    return u64(moved<CTRL, ROWS>(uint32_t(old), uint32_t(v))) |
+           u64(moved<CTRL, ROWS>(uint32_t(old >> 32), uint32_t(v >> 32))) << 32;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float old, float v) {
+    return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(old), __float_as_uint(v)));
+}
+// f(... f(first, second) ..., this lane's); `none`: what f leaves as it is
+template <typename S, typename F>
+__device__ __forceinline__ S wave_scan(S v, S none, F f) {
+    v = f(v, moved<0x111, 0xf>(none, v));   // from 1, 2, 4, 8 lanes before in the row
+    v = f(v, moved<0x112, 0xf>(none, v));
+    v = f(v, moved<0x114, 0xf>(none, v));
+    v = f(v, moved<0x118, 0xf>(none, v));
+    v = f(v, moved<0x142, 0xa>(none, v));   // the row's last to the next row (rows 1 and 3)
+    v = f(v, moved<0x143, 0xc>(none, v));   // lane 31 to the upper half
+    return v;
+}
+__device__ __forceinline__ u64 up_to(u64 v) { return wave_scan(v, u64(0), [](u64 a, u64 b) { return a + b; }); }
+__device__ __forceinline__ uint32_t up_to(uint32_t v) { return wave_scan(v, 0u, [](uint32_t a, uint32_t b) { return a + b; }); }
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return uint32_t(__builtin_amdgcn_readlane(int(v), 63)); }
+__device__ __forceinline__ u64 last_lane(u64 v) { return u64(last_lane(uint32_t(v))) | u64(last_lane(uint32_t(v >> 32))) << 32; }
+__device__ __forceinline__ float last_lane(float v) { return __uint_as_float(last_lane(__float_as_uint(v))); }
+__device__ __forceinline__ float wave_max(float v) {
+    return last_lane(wave_scan(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); }));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    return last_lane(wave_scan(v, 0.f, [](float a, float b) { return a + b; }));
 }
 
 template <typename T>

@@ -47,45 +47,6 @@ struct SampleArgs {
     int32_t* kept;
 };
 
-typedef unsigned long long u64;
-
-// ---- sums, scans and maxima over a wave, by moves between neighbouring lanes and rows of 16
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t moved(uint32_t old, uint32_t v) {
-    return uint32_t(__builtin_amdgcn_update_dpp(int(old), int(v), CTRL, ROWS, 0xf, false));
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 moved(u64 old, u64 v) {
-    return u64(moved<CTRL, ROWS>(uint32_t(old), uint32_t(v))) |
-           u64(moved<CTRL, ROWS>(uint32_t(old >> 32), uint32_t(v >> 32))) << 32;
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float moved(float old, float v) {
-    return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(old), __float_as_uint(v)));
-}
-// f(... f(first, second) ..., this lane's); `none`: what f leaves as it is
-template <typename S, typename F>
-__device__ __forceinline__ S wave_scan(S v, S none, F f) {
-    v = f(v, moved<0x111, 0xf>(none, v));   // from 1, 2, 4, 8 lanes before in the row
-    v = f(v, moved<0x112, 0xf>(none, v));
-    v = f(v, moved<0x114, 0xf>(none, v));
-    v = f(v, moved<0x118, 0xf>(none, v));
-    v = f(v, moved<0x142, 0xa>(none, v));   // the row's last to the next row (rows 1 and 3)
-    v = f(v, moved<0x143, 0xc>(none, v));   // lane 31 to the upper half
-    return v;
-}
-__device__ __forceinline__ u64 up_to(u64 v) { return wave_scan(v, u64(0), [](u64 a, u64 b) { return a + b; }); }
-__device__ __forceinline__ uint32_t up_to(uint32_t v) { return wave_scan(v, 0u, [](uint32_t a, uint32_t b) { return a + b; }); }
-__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return uint32_t(__builtin_amdgcn_readlane(int(v), 63)); }
-__device__ __forceinline__ u64 last_lane(u64 v) { return u64(last_lane(uint32_t(v))) | u64(last_lane(uint32_t(v >> 32))) << 32; }
-__device__ __forceinline__ float last_lane(float v) { return __uint_as_float(last_lane(__float_as_uint(v))); }
-__device__ __forceinline__ float wave_max(float v) {
-    return last_lane(wave_scan(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); }));
-}
-__device__ __forceinline__ float wave_sum(float v) {
-    return last_lane(wave_scan(v, 0.f, [](float a, float b) { return a + b; }));
-}
-
 // Order of floats as integers (-0 as 0; no NaN)
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t b = __float_as_uint(x + 0.f);
@@ -145,9 +106,7 @@ struct Weight {
     __device__ __forceinline__ u64 raw(float x) const {
         const double e = fmax((double(x) - m) * c, least);      // (-inf, and NaN from 0 * inf, go to `least`)
         const double z = e + magic, f = e - (z - magic);        // z: e + bits rounded, in its low bits
-        const u64 b = u64(__double_as_longlong(power_of_2(f)));
-        const uint32_t high = uint32_t(b >> 32) + (uint32_t(__double_as_longlong(z)) << 20);
-        return u64(__double_as_longlong(__longlong_as_double((u64(high) << 32) | uint32_t(b)) + 0x1p52));
+        return u64(__double_as_longlong(ldexp(power_of_2(f), int(uint32_t(__double_as_longlong(z)))) + 0x1p52));
     }
     __device__ __forceinline__ u64 operator()(float x) const { return raw(x) - kOne; }
 };
@@ -182,9 +141,9 @@ struct Run {
 };
 
 // Pieces of 16 bytes of a row that LDS holds beside the rest (29 of a CU's 160 KB): in a
-// workgroup of 1024 threads, in one of 256 and in one of 512 (one more where the row starts inside one).
+// workgroup of 1024 threads, in one of 256 and in one of 512.
 constexpr int kHeld = 8192, kHeldSmall = 512, kHeldMiddle = 2048;
-template <int THREADS> constexpr int kSlots = THREADS == 256 ? 2 : THREADS == 512 ? 4 : 8;   // a thread's, in a row of whole pieces
+template <int THREADS> constexpr int kSlots = THREADS == 256 ? 2 : THREADS == 512 ? 4 : 8;   // a thread's at most
 constexpr size_t held_bytes(int64_t np) { return size_t(np + 8) * 16; }  // (the last thread's pieces are turned as well)
 
 // HELD: the row is in LDS, a thread has `slots` pieces one after another; else a wave
@@ -192,14 +151,14 @@ constexpr size_t held_bytes(int64_t np) { return size_t(np + 8) * 16; }  // (the
 template <typename T, int THREADS, bool HELD>
 struct Sampler {
     static constexpr int VEC = 16 / sizeof(T), WAVES = THREADS / 64;
-    const Row<T> row;
+    const T* row;
     Shared<THREADS>& sh;
-    int np, slots, first, turn;
+    int V, np, slots, first, turn;   // V elements in np pieces
     float m = 0.f;
     Weight weight;
 
-    __device__ __forceinline__ Sampler(const T* p, int V, Shared<THREADS>& s) : row(p, V), sh(s) {
-        np = row.pieces();
+    __device__ __forceinline__ Sampler(const T* p, int n, Shared<THREADS>& s) : row(p), sh(s), V(n) {
+        np = (V + VEC - 1) / VEC;
         slots = (np + THREADS - 1) / THREADS;
         first = HELD ? int(threadIdx.x) * slots : int(threadIdx.x >> 6) * slots * 64 + int(threadIdx.x & 63);
         turn = HELD ? turn_of(threadIdx.x) : 0;
@@ -218,13 +177,31 @@ struct Sampler {
     template <typename F>
     __device__ __forceinline__ void elements(const Piece<T>& v, int p, F f) const {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) f(v.get(j), p * VEC + j - row.lo);
+        for (int j = 0; j < VEC; ++j) f(v.get(j), p * VEC + j);
+    }
+    __device__ __forceinline__ bool ragged() const { return V % VEC != 0; }   // the last piece has less
+    // 16 bytes from where any element starts
+    __device__ __forceinline__ uint4 whole_piece(int p) const {
+        typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+        const Words w = *reinterpret_cast<const Words*>(row + int64_t(p) * VEC);
+        return make_uint4(w.x, w.y, w.z, w.w);
+    }
+    // (the last piece may have less: by its elements)
+    __device__ __forceinline__ Piece<T> from_memory(int p) const {
+        Piece<T> r;
+        if (p < np - 1 || !ragged()) {
+            r.v = whole_piece(p);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) r.set(j, p * VEC + j < V ? row[p * VEC + j] : out_f<T>(-INFINITY));
+        }
+        return r;
     }
     __device__ __forceinline__ bool piece(int i, int& p, Piece<T>& v) const {
         p = HELD ? first + i : first + i * 64;
         if (p >= np) return false;
         if constexpr (HELD) v.v = held_row[held_at(first, turn, i)];
-        else v = row.load(p);
+        else v = from_memory(p);
         return true;
     }
     template <typename F>
@@ -240,13 +217,12 @@ struct Sampler {
 #pragma unroll 1
         for (int i = 0; i < slots; ++i) slot(i, f);
     }
-    __device__ __forceinline__ bool pieces_whole() const { return row.lo == 0 && row.hi % VEC == 0; }
-    // The row's pieces tid, tid + THREADS, ... on their way to registers (whole pieces only)
+    // The row's pieces tid, tid + THREADS, ... on their way to registers, but a ragged one
     __device__ __forceinline__ void fetch(uint4 (&v)[kSlots<THREADS>]) const {
-        const uint4* from = reinterpret_cast<const uint4*>(row.base);
+        const int last = V / VEC - 1;
 #pragma unroll
         for (int k = 0; k < kSlots<THREADS>; ++k)
-            if (k < slots) v[k] = from[min(int(threadIdx.x) + k * THREADS, np - 1)];
+            if (k < slots && last >= 0) v[k] = whole_piece(min(int(threadIdx.x) + k * THREADS, last));
     }
     // The first pass, which brings the row to LDS (any thread meets any element): the
     // largest of what the thread met, and whether any was NaN, and any -inf (or may be).
@@ -267,23 +243,21 @@ struct Sampler {
             }
         };
         if constexpr (HELD) {
-            const uint32_t inv = ((1u << 18) + slots - 1) / slots;   // (exact for p up to 8192, slots up to 9)
+            const uint32_t inv = ((1u << 18) + slots - 1) / slots;   // (exact for p up to 8192, slots up to 8)
             auto put = [&](const Piece<T>& x, int p) {
-                const int t = int(uint32_t(p) * inv >> 18), i = p - t * slots;
-                held_row[held_at(t * slots, turn_of(t), i)] = x.v;
+                const int t = int(__umul24(uint32_t(p), inv) >> 18), i = p - int(__umul24(uint32_t(t), uint32_t(slots)));
+                held_row[held_at(p - i, turn_of(t), i)] = x.v;
                 meet(x);
             };
-            if (pieces_whole()) {
+            const int full = V / VEC;
 #pragma unroll
-                for (int k = 0; k < kSlots<THREADS>; ++k) {
-                    const int p = int(threadIdx.x) + k * THREADS;
-                    Piece<T> x;
-                    x.v = v[k];
-                    if (k < slots && p < np) put(x, p);
-                }
-            } else {
-                for (int p = threadIdx.x; p < np; p += THREADS) put(row.load(p), p);
+            for (int k = 0; k < kSlots<THREADS>; ++k) {
+                const int p = int(threadIdx.x) + k * THREADS;
+                Piece<T> x;
+                x.v = v[k];
+                if (k < slots && p < full) put(x, p);
             }
+            if (ragged() && int(threadIdx.x) == full % THREADS) put(from_memory(full), full);
         } else {
 #pragma unroll 1
             for (int i = 0; i < slots; ++i) {
@@ -335,7 +309,7 @@ struct Sampler {
             const int t = sh.at, start = t * slots, n = min(slots, np - start) * VEC, turned = turn_of(t);
             u64 left = target - sh.before;
             for (int e0 = 0; e0 < n; e0 += 64) {
-                const int e = e0 + lane, j = start * VEC + e - row.lo;
+                const int e = e0 + lane, j = start * VEC + e;
                 float x = -INFINITY;
                 if (e < n) {
                     const T* at = reinterpret_cast<const T*>(&held_row[held_at(start, turned, e / VEC)]);
@@ -619,9 +593,9 @@ struct Sampler {
     // the thread's element of a bit, and its index
     __device__ __forceinline__ float marked(int bit, int& index) const {
         const int i = bit / VEC, j = bit % VEC, p = HELD ? first + i : first + i * 64;
-        index = p * VEC + j - row.lo;
+        index = p * VEC + j;
         if constexpr (HELD) return to_f(reinterpret_cast<const T*>(&held_row[held_at(first, turn, i)])[j]);
-        else return to_f(row.base[p * VEC + j]);
+        else return to_f(row[index]);
     }
     __device__ __forceinline__ bool few() const { return slots * VEC <= 64; }   // (a bit is one element)
     // Bins of weights: 1/32 of a power of two each, the last one all below 2^-32
@@ -690,7 +664,7 @@ struct Sampler {
 
 template <typename T, int THREADS, bool HELD>
 __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREADS, HELD>& s, Shared<THREADS>& sh, int r,
-                                           uint4 (&pieces)[kSlots<THREADS>], bool more) {
+                                           bool more) {
     constexpr int WAVES = THREADS / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float temp = a.T_ ? a.T_[r] : a.T, p = a.p_ ? a.p_[r] : a.p, minp = a.minp_ ? a.minp_[r] : a.minp, u = a.u[r];
@@ -705,10 +679,18 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
     // the largest logit of the thread and of the row, the smallest of the threads' largest
     float own;
     bool nan, holes;
-    s.largest(pieces, own, nan, holes);
-    if (more) {   // the next row is on its way while this one is worked on
-        const Sampler<T, THREADS, HELD> after(static_cast<const T*>(a.logits) + (r + int64_t(gridDim.x)) * a.ld, a.V, sh);
-        if (after.pieces_whole()) after.fetch(pieces);
+    {
+        uint4 pieces[kSlots<THREADS>];
+        if (HELD) s.fetch(pieces);
+        s.largest(pieces, own, nan, holes);
+    }
+    // The next row comes nearer while this one is worked on: a thread touches one line of 128 bytes
+    // (in registers of its own the row took those of the work on this one).
+    uint32_t touched = 0;
+    if (more) {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(static_cast<const T*>(a.logits) + (r + int64_t(gridDim.x)) * a.ld);
+        const uintptr_t at = ((from + 127) & ~uintptr_t(127)) + size_t(tid) * 128;
+        if (at + 4 <= from + size_t(a.V) * sizeof(T)) touched = *reinterpret_cast<const uint32_t*>(at);
     }
     float m = wave_max(own), low = wave_max(own > -INFINITY ? -own : -INFINITY);
     nan = __ballot(nan) != 0, holes = __ballot(holes) != 0;
@@ -741,6 +723,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
     const bool exps = a.logp && !(sum_all && temp == 1.f);
     const bool bins = sum_all && part && !some;
     const auto g = s.gather(exps, sum_all, sum_all && a.kept && holes, bins, least);
+    asm volatile("" ::"v"(touched));
     u64 mine = g.mine;
     uint32_t live = holes ? g.live : uint32_t(a.V);
     // sums of all, and of the threads before
@@ -870,7 +853,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
                 int p;
                 Piece<T> v;
                 if (!s.piece(i, p, v)) break;
-                int j = p * Sampler<T, THREADS, HELD>::VEC - s.row.lo;
+                int j = p * Sampler<T, THREADS, HELD>::VEC;
                 marks |= u64(s.mark(v, [&](float x) { return kept(x, j++); })) << (i * Sampler<T, THREADS, HELD>::VEC);
             }
             live = uint32_t(__popcll(marks));
@@ -900,11 +883,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
 template <typename T, int THREADS, bool HELD>
 __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a) {
     __shared__ Shared<THREADS> sh;
-    uint4 pieces[kSlots<THREADS>];   // the next row's
     for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
         Sampler<T, THREADS, HELD> s(static_cast<const T*>(a.logits) + r * a.ld, a.V, sh);
-        if (HELD && r == int(blockIdx.x) && s.pieces_whole()) s.fetch(pieces);
-        sample_row(a, s, sh, r, pieces, HELD && int64_t(r) + gridDim.x < a.rows);
+        sample_row(a, s, sh, r, HELD && int64_t(r) + gridDim.x < a.rows);
         __syncthreads();   // (the row in LDS and the lists are done with)
     }
 }
@@ -938,7 +919,7 @@ janus_status sample_launch(const SampleArgs& a, int64_t np, hipStream_t st) {
         std::lock_guard<std::mutex> guard(lock);
         if (!told[dev])
             JANUS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(sample_kernel<T, THREADS, HELD>),
-                                          hipFuncAttributeMaxDynamicSharedMemorySize, int(held_bytes(kHeld + 1))));
+                                          hipFuncAttributeMaxDynamicSharedMemorySize, int(held_bytes(kHeld))));
         told[dev] = true;
     }
     // 16 waves on a CU: what a workgroup of 1024 threads fills
@@ -949,10 +930,10 @@ janus_status sample_launch(const SampleArgs& a, int64_t np, hipStream_t st) {
 }
 template <typename T>
 janus_status sample_dispatch(const SampleArgs& a, hipStream_t st) {
-    const int64_t full = (int64_t(a.V) * sizeof(T) + 15) / 16, np = full + 1;   // (a row may start inside a piece)
-    if (full <= kHeldSmall) return sample_launch<T, 256, true>(a, np, st);
-    if (full <= kHeldMiddle) return sample_launch<T, 512, true>(a, np, st);
-    if (full <= kHeld) return sample_launch<T, 1024, true>(a, np, st);
+    const int64_t np = (int64_t(a.V) * sizeof(T) + 15) / 16;
+    if (np <= kHeldSmall) return sample_launch<T, 256, true>(a, np, st);
+    if (np <= kHeldMiddle) return sample_launch<T, 512, true>(a, np, st);
+    if (np <= kHeld) return sample_launch<T, 1024, true>(a, np, st);
     return sample_launch<T, 1024, false>(a, np, st);
 }
 
