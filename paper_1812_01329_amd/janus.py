@@ -656,14 +656,23 @@ def janus_sgd_clip_update_noalloc(desc: SgdDesc, params, grads, stats=None, stre
 def adamw_tensors(params, grads, m, v, scale=None, master=None, decay=0.0) -> C.Array:
     """The tensors of janus_adamw_update, as it takes them: lists of device
     tensors (``scale`` of 8-bit states; ``master`` with None where a parameter has
-    none), ``decay`` one number or one for each.  Made once for an update's every step."""
+    none), ``decay`` one number or one for each.  Made once for an update's every step.
+    Raises ValueError where sizes or types do not go together."""
     import torch
     n = len(params)
     out = (AdamWTensor * n)()
+    state = torch.float32 if scale is None else (torch.uint8, torch.float8_e4m3fn)
     for i in range(n):
         w = None if master is None else master[i]
+        size, f32 = params[i].numel(), torch.float32
+        for name, t, dts, least in (("p", params[i], (f32, torch.bfloat16), size), ("g", grads[i], f32, size), ("m", m[i], state, size),
+                                    ("v", v[i], state, size), ("master", w, f32, size),
+                                    ("scale", None if scale is None else scale[i], f32, -(-size // 256) * 2)):
+            if t is not None and (t.numel() != least or not t.is_contiguous() or
+                                  t.dtype not in (dts if isinstance(dts, tuple) else (dts,))):
+                raise ValueError(f"adamw_tensors: {name} of tensor {i}: {t.dtype} {tuple(t.shape)} for {size} parameters")
         out[i] = AdamWTensor(_p(params[i]), _p(grads[i]), _p(m[i]), _p(v[i]), None if scale is None else _p(scale[i]), _p(w),
-                             params[i].numel(), float(decay if np.isscalar(decay) else decay[i]),
+                             size, float(decay if np.isscalar(decay) else decay[i]),
                              BF16 if params[i].dtype == torch.bfloat16 else F32)
     out.tensors = [t for ts in (params, grads, m, v, scale or [], master or []) for t in ts if t is not None]   # (kept alive)
     devices = {t.get_device() for t in out.tensors}

@@ -75,7 +75,9 @@ class AdamW:
 class AdamWUpdate:
     """The AdamW update that ends a training step (janus_adamw_update): every
     parameter tensor with its float32 gradient, float32 and bf16 parameters in one
-    call under one norm."""
+    call under one norm.  Master copies are taken of the parameters as they are
+    when the update is made (or from a state dict): parameters that are set later
+    need an update of their own."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], spec: AdamW):
         if spec.bits not in (8, 32):

@@ -199,3 +199,16 @@ def test_host_tensors_are_refused():
     from paper_1812_01329_amd import train_step as ts
     with pytest.raises(ValueError, match="not on the GPU"):
         ts.make_update([x], [x.clone()], ts.AdamW(1e-3)).apply()
+
+
+def test_tensors_that_do_not_go_together():
+    import torch
+    z = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt)
+    good = dict(params=[z(300)], grads=[z(300)], m=[z(300, torch.uint8)], v=[z(300, torch.uint8)], scale=[torch.zeros(2, 2)])
+    J.adamw_tensors(**good)
+    for name, bad in (("grads", z(299)), ("grads", z(300, torch.bfloat16)), ("params", z(300, torch.float16)), ("m", z(300)),
+                      ("v", z(301, torch.uint8)), ("scale", torch.zeros(1, 2)), ("params", z(600)[::2]), ("master", z(3))):
+        with pytest.raises(ValueError, match="adamw_tensors"):
+            J.adamw_tensors(**{**good, name: [bad]})
+    with pytest.raises(ValueError, match="adamw_tensors"):
+        J.adamw_tensors([z(3)], [z(3)], [z(3, torch.uint8)], [z(3)])   # no scale: states of 32 bits
