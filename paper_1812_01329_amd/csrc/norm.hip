@@ -487,9 +487,11 @@ void fwd_vec(const NormArgs& a, hipStream_t st) {
 template <typename T, int VEC, int LANES, int P>
 int bwd_launch(const NormArgs& a, hipStream_t st) {
     constexpr int THREADS = LANES > kBwdThreads ? LANES : kBwdThreads, ROWS = THREADS / LANES;
-    // (a workgroup's sums cost as much as three or four rows)
+    // A workgroup's sums cost as much as three or four rows, but few rows spread over the
+    // CUs gain more: 64 at least instead of 256 takes 11.2 us instead of 9.9 for 1500 rows of
+    // 301 float32 and 13.9 instead of 12.9 for 1500 of 2048 bf16.
     const int64_t groups = (int64_t(a.rows) + ROWS - 1) / ROWS;
-    const int blocks = int(std::min<int64_t>(groups, std::min<int64_t>(std::max<int64_t>(64, groups / 4), kNormBlocks)));
+    const int blocks = int(std::min<int64_t>(groups, std::min<int64_t>(std::max<int64_t>(256, groups / 4), kNormBlocks)));
     hipLaunchKernelGGL((norm_bwd_kernel<T, VEC, LANES, P>), dim3(blocks), dim3(THREADS), 0, st, a);
     return blocks;
 }
