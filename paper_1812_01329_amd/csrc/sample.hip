@@ -726,6 +726,18 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
     asm volatile("" ::"v"(touched));
     u64 mine = g.mine;
     uint32_t live = holes ? g.live : uint32_t(a.V);
+    auto add_marked = [&](u64 marks) {
+        mine = 0, live = uint32_t(__popcll(marks));
+        for (; marks; marks &= marks - 1) {
+            int j;
+            mine += s.weight(s.marked(__ffsll(marks) - 1, j));
+        }
+    };
+    // With min-p alone nothing has to be ranked: the marked weights are added up where they are
+    // (2000 rows of 1000 bf16 logits, min_p 0.05: 14.6 us, through a list 32.5; 2000 of 32768: 72 and 150).
+    // A mark of two elements would be looked at again: the list is no slower then where it is short.
+    const bool marked = least > -INFINITY && some && k <= 0 && !part && s.few();
+    if (marked) add_marked(g.marks);
     // sums of all, and of the threads before
     u64 all = 0, before = 0;
     if (sum_all) {
@@ -748,7 +760,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
         return min(fraction(chance, sum, cut), sum - 1);
     };
 
-    if (least > -INFINITY) {
+    if (least > -INFINITY && !marked) {
         s.list(least, g.marks);
         const int n = int(sh.n);
         if (greedy && n <= kPairs) {   // the first of the largest
@@ -845,8 +857,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
 
     auto kept = [&](float x, int j) { return x > -INFINITY && run.has(key_of(x), j); };
     if (!sum_all || part) {   // (else added up already)
-        mine = 0, live = 0;
-        if (s.few()) {   // a fifth of the row or so: its weights alone
+        if (!marked && s.few()) {   // a fifth of the row or so: its weights alone
             u64 marks = 0;
 #pragma unroll 1
             for (int i = 0; i < s.slots; ++i) {
@@ -856,12 +867,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
                 int j = p * Sampler<T, THREADS, HELD>::VEC;
                 marks |= u64(s.mark(v, [&](float x) { return kept(x, j++); })) << (i * Sampler<T, THREADS, HELD>::VEC);
             }
-            live = uint32_t(__popcll(marks));
-            for (; marks; marks &= marks - 1) {
-                int j;
-                mine += s.weight(s.marked(__ffsll(marks) - 1, j));
-            }
-        } else {
+            add_marked(marks);
+        } else if (!marked) {
+            mine = 0, live = 0;
             s.each([&](float x, int j) {
                 const u64 w = s.weight(x);
                 const bool in = kept(x, j);
