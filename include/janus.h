@@ -831,7 +831,8 @@ typedef struct {
     float top_p, min_p;     /* not NaN */
 } janus_sample_desc;
 
-/* Bytes of workspace of janus_sample (0 for a bad descriptor; may be 0). */
+/* Bytes of workspace of janus_sample: 0, a row stays on its compute unit or is read
+ * again (ws may be NULL). */
 size_t janus_sample_workspace_bytes(const janus_sample_desc* d);
 
 /*
@@ -846,7 +847,7 @@ size_t janus_sample_workspace_bytes(const janus_sample_desc* d);
  *  kept     int32 [rows] or NULL: how many tokens were kept.
  * Errors: NULL d/logits/u/tokens, a non-positive size, ld below V, a temperature
  * that is negative, or a NaN in d, a pointer not aligned to its element -> INVALID_ARG;
- * dtype not F32/BF16, V past 2^24, rows past 2^30 -> UNSUPPORTED; WORKSPACE.
+ * dtype not F32/BF16, V past 2^24, rows past 2^30 -> UNSUPPORTED.
  */
 janus_status janus_sample(const janus_sample_desc* d, const void* logits, const float* u,
                           const float* temperature, const int32_t* top_k, const float* top_p,

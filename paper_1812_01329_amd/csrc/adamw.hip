@@ -18,6 +18,11 @@
 // of the mantissa to 3 bits, which adds 16 random bits below them and cuts off.
 // sqrt(v) is kept in v's place: its range is half of v's in powers of two (e4m3
 // reaches 2^-18 of the largest), and half of v's relative step.
+//
+// 19.8 M float32 parameters with 32-bit states: the norm 14.7 us (5.4 TB/s, partly from
+// the cache), the update 88 (6.3 TB/s with gradients in the cache; 108 us a call, where a
+// copy of the same bytes takes 117).  71 M of bf16 with masters and 8-bit states: 45 and 210 us
+// (255 a call, 273).  10 small tensors: 3.2 and 4.7 us, latency.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -207,7 +212,8 @@ struct Step {
 // loads go out without a branch between them; PAST, one access that starts at a multiple of its
 // size and goes past the caches: what the update reads and writes is not met again before the next step, and leaves the gradients of the first
 // pass their place (19.8 M float32 parameters: 108 us a call, 130 without; 71 M
-// of bf16 with masters and 8-bit states 269 and 320; the first pass's own loads: slower so).
+// of bf16 with masters and 8-bit states 269 and 320 when it was tried; the first pass's own
+// loads: slower so).
 enum How { SOME, ALL, PAST };
 template <typename T> struct Access;
 template <> struct Access<float> {
@@ -476,6 +482,8 @@ size_t adamw_carve(AdamArgs& a, Tensors& t, int n, void* ws) {
 }
 
 // Calls of up to this many elements are cut in tiles of 1024, for there to be more of them.
+// With tiles of 1024 and of 4096: 2^18 elements 8.0 and 9.4 us (8-bit states 8.5 and 12.7),
+// 2^21 16.6 and 16.7 (16.7 and 15.5), 2^22 29.6 and 26.5 (26.3 and 22.2).
 constexpr int64_t kSmallTotal = 1 << 21;
 
 // The two passes, over a table by value or in the workspace

@@ -13,6 +13,11 @@
 // second kernel adds them up in their order.  Everything between loads and stores is
 // float32; the variance is that of the differences from the mean (a mean of squares
 // less the square of the mean loses what a large mean has in common).
+//
+// Bound by memory: training 65536 rows of 2048 bf16 with a residual, the forward takes
+// 201 us (5.3 TB/s of four tensors) and the backward 215 (5.0 TB/s); 25600 rows of 1024 27
+// and 32 us, partly from the last-level cache.  Few rows are bound by latency: 20 rows of
+// 1300 take 3.8 us, 1021 of 301 float32 4.2 and 4.9.
 #include <cmath>
 
 #include "rows.hpp"
@@ -183,8 +188,9 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
     }
 }
 
-// As the forward; a workgroup takes every gridDim.x-th group of rows.  P = 0: dx
-// alone, by two reads of a row.
+// As the forward; a workgroup takes every gridDim.x-th group of rows.  65536 rows of 2048
+// bf16 take 215 us, a row in 256 threads; with a row in a wave, 32 elements a thread, 305
+// (registers leave too few waves).  P = 0: dx alone, by two reads of a row.
 constexpr int kBwdThreads = 512;   // (the fewer workgroups, the fewer sums of dgamma and dbeta)
 template <typename T, int VEC, int LANES, int P>
 __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void norm_bwd_kernel(NormArgs a) {
@@ -346,7 +352,8 @@ __global__ __launch_bounds__(kThreads) void norm_cols_kernel(NormArgs a) {
 }
 
 // The workgroups' sums, added up: 64 columns of dgamma or dbeta a workgroup, four of
-// them and every 64th sum a thread.
+// them and every 64th sum a thread.  512 sums of 2048 columns take 4.2 us, 1024 of them 23
+// and 2048 48: why the backward has 512 workgroups at most.
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* part, int n, int D, float* dgamma, float* dbeta) {
     __shared__ float4 red[64][16];
     const int col = threadIdx.x & 15, from = threadIdx.x >> 4;
