@@ -985,7 +985,7 @@ typedef struct {
     janus_adamw_states states;
     float lr;               /* finite */
     float beta1, beta2;     /* in [0, 1) */
-    float eps;              /* finite, > 0 */
+    float eps;              /* finite, at least 2^-126 (its reciprocal stays finite) */
     float max_norm;         /* as in janus_sgd_desc */
     uint32_t seed;          /* of the 8-bit states' rounding */
 } janus_adamw_desc;

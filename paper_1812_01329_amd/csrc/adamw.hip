@@ -204,7 +204,8 @@ struct Step {
         v = v * b2 + (g * g) * c2;
     }
     __device__ __forceinline__ float parameter(float p, float m, float r) const {
-        return p - p * shrink - rate * m * __builtin_amdgcn_rcpf(r * root + eps);   // (off by an ulp of the step)
+        // (off by an ulp of the step; eps is 2^-126 at least, whose reciprocal is finite)
+        return p - p * shrink - rate * (m * __builtin_amdgcn_rcpf(r * root + eps));
     }
 };
 
@@ -293,6 +294,12 @@ __device__ __forceinline__ float root_of(float v) {
     // the borders are the squares of the means: (s - ulp / 2)^2 = s down + ulp^2 / 4
     if (fmaf(-down, s, v) <= 0.f) return down;
     return fmaf(-up, s, v) > 0.f ? up : s;
+}
+
+// sqrt v to an ulp; the instruction takes subnormal ones for 0
+__device__ __forceinline__ float near_root(float v) {
+    const bool low = v < 0x1p-96f;
+    return __builtin_amdgcn_sqrtf(low ? v * 0x1p64f : v) * (low ? 0x1p-32f : 1.f);
 }
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -399,7 +406,7 @@ struct Four {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 st.moments(g[j], m[j], v[j]);
-                r[j] = __builtin_amdgcn_sqrtf(v[j]);
+                r[j] = near_root(v[j]);
             }
             store4<HOW>(static_cast<float*>(t.m) + e, k, m);
             store4<HOW>(static_cast<float*>(t.v) + e, k, v);
@@ -505,7 +512,7 @@ janus_status adamw_run(const Table& t, const AdamArgs& a, bool small, double tot
 
 bool adamw_desc_ok(const janus_adamw_desc* d) {
     return d && d->n >= 1 && std::isfinite(d->lr) && d->beta1 >= 0.f && d->beta1 < 1.f && d->beta2 >= 0.f &&
-           d->beta2 < 1.f && std::isfinite(d->eps) && d->eps > 0.f && !std::isnan(d->max_norm);
+           d->beta2 < 1.f && std::isfinite(d->eps) && d->eps >= 0x1p-126f && !std::isnan(d->max_norm);
 }
 
 janus_status adamw_check(const janus_adamw_desc* d, const janus_adamw_tensor* tensors) {

@@ -140,6 +140,12 @@ def test_adamw_descriptors(change, status):
     call(status, d)
 
 
+def test_adamw_eps_is_a_normal_number():
+    """The reciprocal of a smaller one leaves float32: 0 / (0 + eps) would be NaN."""
+    assert J.janus_adamw_workspace_bytes(adamw(eps=2.0 ** -127)) == 0
+    assert J.janus_adamw_workspace_bytes(adamw(eps=2.0 ** -126)) > 0
+
+
 def test_adamw_arguments():
     d = adamw()
     call(INV, d, "none")
