@@ -65,23 +65,57 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float* red) {
     }
 }
 
-template <int VEC>
-__device__ __forceinline__ void load_f(const float* p, float* f) {
-    if constexpr (VEC % 4 == 0) {
-#pragma unroll
-        for (int j = 0; j < VEC; j += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(p + j);
-            f[j] = v.x, f[j + 1] = v.y, f[j + 2] = v.z, f[j + 3] = v.w;
+// VEC elements at p.  ODD: wherever they start, and of the last ones only `left` are there (the
+// others are read as 0).
+template <typename T, int VEC, bool ODD>
+struct Span {
+    Chan<T, VEC> c;
+    __device__ __forceinline__ void load(const T* p, int left) {
+        if constexpr (!ODD) {
+            c.load(p);
+        } else if (left >= VEC) {
+            __builtin_memcpy(&c.v, p, sizeof(c.v));
+        } else if constexpr (sizeof(T) == 2) {
+            c.v = make_uint2(word(p, 0, left), word(p, 2, left));
+        } else {
+            c.v = make_float4(p[0], left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, 0.f);
         }
-    } else {
+    }
+    __device__ __forceinline__ void get(float* f) const { c.get(f); }
+    __device__ __forceinline__ static void store(T* p, const float* f, int left) {
+        if constexpr (!ODD) {
+            Chan<T, VEC>::store(p, f);
+        } else if (left >= VEC) {
+            Chan<T, VEC> o;
+            if constexpr (sizeof(T) == 2) o.v = make_uint2(pack2(f[0], f[1]), pack2(f[2], f[3]));
+            else o.v = make_float4(f[0], f[1], f[2], f[3]);
+            __builtin_memcpy(p, &o.v, sizeof(o.v));
+        } else {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) f[j] = p[j];
+            for (int j = 0; j < VEC; ++j)
+                if (j < left) p[j] = out_f<T>(f[j]);
+        }
+    }
+
+  private:
+    __device__ __forceinline__ static uint32_t word(const T* p, int j, int left) {
+        return (j < left ? uint32_t(p[j]) : 0u) | (j + 1 < left ? uint32_t(p[j + 1]) << 16 : 0u);
+    }
+};
+template <int VEC, bool ODD>
+__device__ __forceinline__ void load_f(const float* p, float* f, int left) {
+    constexpr int ONE = VEC < 4 ? 1 : 4;
+#pragma unroll
+    for (int j = 0; j < VEC; j += ONE) {
+        Span<float, ONE, ODD> v;
+        v.load(p + j, left);
+        v.get(f + j);
     }
 }
 
 // LANES threads a row, P accesses of VEC elements each; P = 0: rows longer than that,
 // read three times (for the mean, the variance, the result).
-template <typename T, int VEC, int LANES, int P>
+template <typename T, int VEC, bool ODD, int LANES, int P>
 __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_kernel(NormArgs a) {
     constexpr int THREADS = LANES > kThreads ? LANES : kThreads, ROWS = THREADS / LANES;
     __shared__ float red[THREADS / 64];
@@ -94,12 +128,12 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
     T* h = a.h && there ? static_cast<T*>(a.h) + row * a.ldh : nullptr;
     T* y = static_cast<T*>(a.y) + row * a.ldy;
     auto load = [&](int c, float* f) {
-        Chan<T, VEC> v;
-        v.load(x + c);
+        Span<T, VEC, ODD> v;
+        v.load(x + c, a.D - c);
         v.get(f);
         if (r) {
             float s[VEC];
-            v.load(r + c);
+            v.load(r + c, a.D - c);
             v.get(s);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) f[j] = to_f(out_f<T>(f[j] + s[j]));
@@ -110,16 +144,16 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
 #pragma unroll
         for (int j = 0; j < VEC; ++j) o[j] = (f[j] - mean) * rstd;
         if (a.gamma) {
-            load_f<VEC>(a.gamma + c, g);
+            load_f<VEC, ODD>(a.gamma + c, g, a.D - c);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) o[j] *= g[j];
         }
         if (a.beta) {
-            load_f<VEC>(a.beta + c, g);
+            load_f<VEC, ODD>(a.beta + c, g, a.D - c);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) o[j] += g[j];
         }
-        if (there) Chan<T, VEC>::store(y + c, o);
+        if (there) Span<T, VEC, ODD>::store(y + c, o, a.D - c);
     };
     float s[1] = {0.f}, q[1] = {0.f};
     if constexpr (P > 0) {
@@ -144,7 +178,8 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
         for (int i = 0; i < P; ++i)
             if ((tid + i * LANES) * VEC < a.D)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) q[0] = fmaf(v[i][j] - mean, v[i][j] - mean, q[0]);
+                for (int j = 0; j < VEC; ++j)
+                    if (!ODD || (tid + i * LANES) * VEC + j < a.D) q[0] = fmaf(v[i][j] - mean, v[i][j] - mean, q[0]);
         row_sum<LANES>(q, red);
         const float rstd = 1.f / sqrtf(q[0] / a.width + a.eps);
         if (tid == 0 && there) {
@@ -155,7 +190,7 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
         for (int i = 0; i < P; ++i) {
             const int c = (tid + i * LANES) * VEC;
             if (c < a.D) {
-                if (h) Chan<T, VEC>::store(h + c, v[i]);
+                if (h) Span<T, VEC, ODD>::store(h + c, v[i], a.D - c);
                 result(c, v[i], mean, rstd);
             }
         }
@@ -172,7 +207,8 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
         for (int64_t c = int64_t(tid) * VEC; c < end; c += LANES * VEC) {
             load(c, v);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) q[0] = fmaf(v[j] - mean, v[j] - mean, q[0]);
+            for (int j = 0; j < VEC; ++j)
+                if (!ODD || c + j < end) q[0] = fmaf(v[j] - mean, v[j] - mean, q[0]);
         }
         row_sum<LANES>(q, red);
         const float rstd = 1.f / sqrtf(q[0] / a.width + a.eps);
@@ -182,7 +218,7 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
         }
         for (int64_t c = int64_t(tid) * VEC; c < end; c += LANES * VEC) {
             load(c, v);   // (before h is written: h may be r or x)
-            if (h) Chan<T, VEC>::store(h + c, v);
+            if (h) Span<T, VEC, ODD>::store(h + c, v, int(end - c));
             result(c, v, mean, rstd);
         }
     }
@@ -192,7 +228,7 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
 // bf16 take 215 us, a row in 256 threads; with a row in a wave, 32 elements a thread, 305
 // (registers leave too few waves).  P = 0: dx alone, by two reads of a row.
 constexpr int kBwdThreads = 512;   // (the fewer workgroups, the fewer sums of dgamma and dbeta)
-template <typename T, int VEC, int LANES, int P>
+template <typename T, int VEC, bool ODD, int LANES, int P>
 __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void norm_bwd_kernel(NormArgs a) {
     constexpr int THREADS = LANES > kBwdThreads ? LANES : kBwdThreads, ROWS = THREADS / LANES, E = P * VEC;
     __shared__ float red[2 * THREADS / 64];
@@ -205,11 +241,11 @@ __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void nor
             const T* h = static_cast<const T*>(a.x) + row * a.ldh;
             const T* dy = static_cast<const T*>(a.dy) + row * a.ldy;
             const float mean = a.mean[row], rstd = a.rstd[row];
-            Chan<T, VEC> hv[P], dv[P];
+            Span<T, VEC, ODD> hv[P], dv[P];
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 const int c = (tid + i * LANES) * VEC;
-                if (c < a.D) hv[i].load(h + c), dv[i].load(dy + c);
+                if (c < a.D) hv[i].load(h + c, a.D - c), dv[i].load(dy + c, a.D - c);
             }
             float xh[P][VEC], g[P][VEC], s[2] = {0.f, 0.f};
 #pragma unroll
@@ -219,7 +255,7 @@ __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void nor
                     hv[i].get(xh[i]);
                     dv[i].get(g[i]);
                     float w[VEC];
-                    if (a.gamma) load_f<VEC>(a.gamma + c, w);
+                    if (a.gamma) load_f<VEC, ODD>(a.gamma + c, w, a.D - c);
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
                         xh[i][j] = (xh[i][j] - mean) * rstd;
@@ -246,14 +282,14 @@ __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void nor
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) o[j] = (g[i][j] - m0 - xh[i][j] * m1) * rstd;
                     if (dh) {
-                        Chan<T, VEC> e;
+                        Span<T, VEC, ODD> e;
                         float f[VEC];
-                        e.load(dh + c);
+                        e.load(dh + c, a.D - c);
                         e.get(f);
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) o[j] += f[j];
                     }
-                    Chan<T, VEC>::store(dx + c, o);
+                    Span<T, VEC, ODD>::store(dx + c, o, a.D - c);
                 }
             }
         }
@@ -294,16 +330,17 @@ __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void nor
         const float mean = a.mean[row], rstd = a.rstd[row];
         float xh[VEC], g[VEC], s[2] = {0.f, 0.f};
         auto load = [&](int64_t c) {
-            Chan<T, VEC> v;
-            v.load(h + c);
+            Span<T, VEC, ODD> v;
+            const int left = int(end - c);
+            v.load(h + c, left);
             v.get(xh);
-            v.load(dy + c);
+            v.load(dy + c, left);
             v.get(g);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) xh[j] = (xh[j] - mean) * rstd;
             if (a.gamma) {
                 float w[VEC];
-                load_f<VEC>(a.gamma + c, w);
+                load_f<VEC, ODD>(a.gamma + c, w, left);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) g[j] *= w[j];
             }
@@ -321,14 +358,14 @@ __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void nor
 #pragma unroll
             for (int j = 0; j < VEC; ++j) o[j] = (g[j] - m0 - xh[j] * m1) * rstd;
             if (dh) {
-                Chan<T, VEC> e;
+                Span<T, VEC, ODD> e;
                 float f[VEC];
-                e.load(dh + c);
+                e.load(dh + c, int(end - c));
                 e.get(f);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) o[j] += f[j];
             }
-            Chan<T, VEC>::store(dx + c, o);
+            Span<T, VEC, ODD>::store(dx + c, o, int(end - c));
         }
     }
 }
@@ -432,7 +469,11 @@ NormArgs norm_args(const janus_norm_desc* d) {
     return a;
 }
 
-// Elements an access: the most that rows' starts and ends allow
+// Elements an aligned access: the most that rows' starts and ends allow.
+// Where that is fewer than four, the forward takes four wherever they start (ODD): 14444 rows of
+// 1409 bf16 27 us, by single elements 64; of 5946, by pairs, 144 and 165; of 1409 float32 34 and 37.
+// The backward does so for single bf16 alone (14444 of 12001: 490 and 935 us): its
+// pairs and its float32 elements are no slower by themselves (5946: 190 and 208 us; 268 and 299).
 int norm_vec(const NormArgs& a, size_t es, std::initializer_list<const void*> rows, std::initializer_list<int64_t> lds) {
     int vec = int(16 / es);
     for (; vec > 1; vec /= 2) {
@@ -446,7 +487,7 @@ int norm_vec(const NormArgs& a, size_t es, std::initializer_list<const void*> ro
 }
 
 // A launch holds fewer than 2^32 threads: more rows take several.
-template <typename T, int VEC, int LANES, int P>
+template <typename T, int VEC, bool ODD, int LANES, int P>
 void fwd_launch(NormArgs a, hipStream_t st) {
     constexpr int THREADS = LANES > kThreads ? LANES : kThreads, ROWS = THREADS / LANES;
     constexpr int64_t kMost = int64_t((1 << 30) / THREADS) * ROWS;
@@ -459,17 +500,17 @@ void fwd_launch(NormArgs a, hipStream_t st) {
         b.y = const_cast<char*>(on(a.y, a.ldy));
         if (a.mean) b.mean = a.mean + r0;
         if (a.rstd) b.rstd = a.rstd + r0;
-        hipLaunchKernelGGL((norm_fwd_kernel<T, VEC, LANES, P>), dim3(unsigned((b.rows + ROWS - 1) / ROWS)), dim3(THREADS), 0,
+        hipLaunchKernelGGL((norm_fwd_kernel<T, VEC, ODD, LANES, P>), dim3(unsigned((b.rows + ROWS - 1) / ROWS)), dim3(THREADS), 0,
                            st, b);
     }
 }
-template <typename T, int VEC, int LANES, int P, int... MORE>
+template <typename T, int VEC, bool ODD, int LANES, int P, int... MORE>
 bool fwd_lanes(const NormArgs& a, int64_t n, hipStream_t st) {
     if (n <= LANES * P) {
-        fwd_launch<T, VEC, LANES, P>(a, st);
+        fwd_launch<T, VEC, ODD, LANES, P>(a, st);
         return true;
     }
-    if constexpr (sizeof...(MORE) > 0) return fwd_lanes<T, VEC, LANES, MORE...>(a, n, st);
+    if constexpr (sizeof...(MORE) > 0) return fwd_lanes<T, VEC, ODD, LANES, MORE...>(a, n, st);
     else return false;
 }
 // From this many rows on a forward gives a bf16 row of up to 2048 elements a wave, which waits for no
@@ -477,21 +518,21 @@ bool fwd_lanes(const NormArgs& a, int64_t n, hipStream_t st) {
 // registers: 25600 of 2048 81 and 73 us).  Fewer rows leave the chip idle that way: 20 rows of 1300
 // take 3.9 us in workgroups of 256, and 5.1.
 constexpr int kWaveRows = 4096;
-template <typename T, int VEC>
+template <typename T, int VEC, bool ODD>
 void fwd_vec(const NormArgs& a, hipStream_t st) {
     const int64_t n = (int64_t(a.D) + VEC - 1) / VEC;   // accesses a row
     constexpr int P = 8 / VEC;
-    if (fwd_lanes<T, VEC, 16, P>(a, n, st)) return;
+    if (fwd_lanes<T, VEC, ODD, 16, P>(a, n, st)) return;
     if constexpr (sizeof(T) == 2)
-        if (a.rows >= kWaveRows && fwd_lanes<T, VEC, 64, P, 2 * P, 4 * P>(a, n, st)) return;
-    if (fwd_lanes<T, VEC, 64, P>(a, n, st) || fwd_lanes<T, VEC, 128, P>(a, n, st) ||
-        fwd_lanes<T, VEC, 256, P>(a, n, st) || fwd_lanes<T, VEC, 512, P>(a, n, st) ||
-        fwd_lanes<T, VEC, 1024, P, 2 * P>(a, n, st))
+        if (a.rows >= kWaveRows && fwd_lanes<T, VEC, ODD, 64, P, 2 * P, 4 * P>(a, n, st)) return;
+    if (fwd_lanes<T, VEC, ODD, 64, P>(a, n, st) || fwd_lanes<T, VEC, ODD, 128, P>(a, n, st) ||
+        fwd_lanes<T, VEC, ODD, 256, P>(a, n, st) || fwd_lanes<T, VEC, ODD, 512, P>(a, n, st) ||
+        fwd_lanes<T, VEC, ODD, 1024, P, 2 * P>(a, n, st))
         return;
-    fwd_launch<T, VEC, 1024, 0>(a, st);
+    fwd_launch<T, VEC, ODD, 1024, 0>(a, st);
 }
 
-template <typename T, int VEC, int LANES, int P>
+template <typename T, int VEC, bool ODD, int LANES, int P>
 int bwd_launch(const NormArgs& a, hipStream_t st) {
     constexpr int THREADS = LANES > kBwdThreads ? LANES : kBwdThreads, ROWS = THREADS / LANES;
     // A workgroup's sums cost as much as three or four rows, but few rows spread over the
@@ -499,29 +540,29 @@ int bwd_launch(const NormArgs& a, hipStream_t st) {
     // 301 float32 and 13.9 instead of 12.9 for 1500 of 2048 bf16.
     const int64_t groups = (int64_t(a.rows) + ROWS - 1) / ROWS;
     const int blocks = int(std::min<int64_t>(groups, std::min<int64_t>(std::max<int64_t>(256, groups / 4), kNormBlocks)));
-    hipLaunchKernelGGL((norm_bwd_kernel<T, VEC, LANES, P>), dim3(blocks), dim3(THREADS), 0, st, a);
+    hipLaunchKernelGGL((norm_bwd_kernel<T, VEC, ODD, LANES, P>), dim3(blocks), dim3(THREADS), 0, st, a);
     return blocks;
 }
-template <typename T, int VEC, int LANES, int P, int... MORE>
+template <typename T, int VEC, bool ODD, int LANES, int P, int... MORE>
 int bwd_lanes(const NormArgs& a, int64_t n, hipStream_t st) {
-    if (n <= LANES * P) return bwd_launch<T, VEC, LANES, P>(a, st);
-    if constexpr (sizeof...(MORE) > 0) return bwd_lanes<T, VEC, LANES, MORE...>(a, n, st);
+    if (n <= LANES * P) return bwd_launch<T, VEC, ODD, LANES, P>(a, st);
+    if constexpr (sizeof...(MORE) > 0) return bwd_lanes<T, VEC, ODD, LANES, MORE...>(a, n, st);
     else return 0;
 }
 // Launches the pass over the rows; returns the number of its sums in a.part.
-template <typename T, int VEC>
+template <typename T, int VEC, bool ODD>
 int bwd_vec(NormArgs a, hipStream_t st) {
     const int64_t n = (int64_t(a.D) + VEC - 1) / VEC;
     int k;
     constexpr int P = 8 / VEC;
-    if ((k = bwd_lanes<T, VEC, 16, P>(a, n, st))) return k;
-    if ((k = bwd_lanes<T, VEC, 64, P>(a, n, st))) return k;
-    if ((k = bwd_lanes<T, VEC, 128, P>(a, n, st))) return k;
-    if ((k = bwd_lanes<T, VEC, 256, P>(a, n, st))) return k;
-    if ((k = bwd_lanes<T, VEC, 512, P>(a, n, st))) return k;
-    if ((k = bwd_lanes<T, VEC, 1024, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, ODD, 16, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, ODD, 64, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, ODD, 128, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, ODD, 256, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, ODD, 512, P>(a, n, st))) return k;
+    if ((k = bwd_lanes<T, VEC, ODD, 1024, P>(a, n, st))) return k;
     if constexpr (sizeof(T) == 2)   // (float32: 404 registers spilled)
-        if ((k = bwd_lanes<T, VEC, 1024, 2 * P>(a, n, st))) return k;
+        if ((k = bwd_lanes<T, VEC, ODD, 1024, 2 * P>(a, n, st))) return k;
     if (a.dx) {   // (a launch holds fewer than 2^32 threads)
         constexpr int64_t kMost = (1 << 30) / 1024;
         const int64_t rows = a.rows, es = sizeof(T);
@@ -532,7 +573,7 @@ int bwd_vec(NormArgs a, hipStream_t st) {
             if (a.dh) b.dh = static_cast<const char*>(a.dh) + r0 * a.ldh * es;
             b.dx = static_cast<char*>(a.dx) + r0 * a.ldx * es;
             b.mean = a.mean + r0, b.rstd = a.rstd + r0;
-            hipLaunchKernelGGL((norm_bwd_kernel<T, VEC, 1024, 0>), dim3(unsigned(b.rows)), dim3(1024), 0, st, b);
+            hipLaunchKernelGGL((norm_bwd_kernel<T, VEC, ODD, 1024, 0>), dim3(unsigned(b.rows)), dim3(1024), 0, st, b);
         }
     }
     if (!a.part) return 0;
@@ -570,14 +611,13 @@ extern "C" janus_status janus_layer_norm_fwd(const janus_norm_desc* d, const voi
     const double el = double(d->rows) * d->D;
     TraceScope trace("norm_fwd", 8.0 * el, el * es * (2 + (r ? 1 : 0) + (h ? 1 : 0)), st);
     if (d->dtype == JANUS_BF16) {
-        if (vec == 8) fwd_vec<bf16_t, 8>(a, st);
-        else if (vec == 4) fwd_vec<bf16_t, 4>(a, st);
-        else if (vec == 2) fwd_vec<bf16_t, 2>(a, st);
-        else fwd_vec<bf16_t, 1>(a, st);
+        if (vec == 8) fwd_vec<bf16_t, 8, false>(a, st);
+        else if (vec == 4) fwd_vec<bf16_t, 4, false>(a, st);
+        else fwd_vec<bf16_t, 4, true>(a, st);
     } else if (vec == 4) {
-        fwd_vec<float, 4>(a, st);
+        fwd_vec<float, 4, false>(a, st);
     } else {
-        fwd_vec<float, 1>(a, st);
+        fwd_vec<float, 4, true>(a, st);
     }
     JANUS_LAUNCH_CHECK();
     return JANUS_OK;
@@ -616,14 +656,14 @@ extern "C" janus_status janus_layer_norm_bwd(const janus_norm_desc* d, const voi
         const double el = double(d->rows) * d->D;
         TraceScope trace("norm_bwd", 14.0 * el, el * es * (2 + (a.dh ? 1 : 0) + (dx ? 1 : 0)), st);
         if (d->dtype == JANUS_BF16) {
-            if (vec == 8) parts = bwd_vec<bf16_t, 8>(a, st);
-            else if (vec == 4) parts = bwd_vec<bf16_t, 4>(a, st);
-            else if (vec == 2) parts = bwd_vec<bf16_t, 2>(a, st);
-            else parts = bwd_vec<bf16_t, 1>(a, st);
+            if (vec == 8) parts = bwd_vec<bf16_t, 8, false>(a, st);
+            else if (vec == 4) parts = bwd_vec<bf16_t, 4, false>(a, st);
+            else if (vec == 2) parts = bwd_vec<bf16_t, 2, false>(a, st);
+            else parts = bwd_vec<bf16_t, 4, true>(a, st);
         } else if (vec == 4) {
-            parts = bwd_vec<float, 4>(a, st);
+            parts = bwd_vec<float, 4, false>(a, st);
         } else {
-            parts = bwd_vec<float, 1>(a, st);
+            parts = bwd_vec<float, 1, false>(a, st);
         }
         JANUS_LAUNCH_CHECK();
     }

@@ -110,6 +110,17 @@ def test_dense(rows, D, dtype):
         c.check()
 
 
+@pytest.mark.parametrize("rows,D", [(4099, 301), (4097, 1027), (4100, 2047), (600, 8195), (530, 12001)])
+def test_many_rows_of_odd_length(rows, D):
+    """Dense bf16 rows that start at odd places, a wave or a workgroup each: accesses
+    wider than their alignment, and a last one that is cut short."""
+    for residual in (False, True):
+        c = Case(rows, D, "bf16", residual=residual, seed=D)
+        c.forward()
+        c.backward()
+        c.check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pads,shift", [((1, 1, 1), 0), ((0, 2, 8), 1), ((8, 8, 8), 8), ((4, 4, 4), 4), ((2, 6, 2), 2),
                                         ((300, 0, 16), 3)])
