@@ -977,6 +977,13 @@ janus_status janus_sgd_clip_update_noalloc(const janus_sgd_desc* d, void* const*
  * the probability that keeps their mean (a step moves v by 0.1 %, which rounding
  * to the nearest of codes 12 % apart would lose), by bits that seed, step, the
  * tensor's place and the element's index decide, so repeated calls give the same result.
+ * A root may so become 0 while the element's m, next to smaller ones, does not: where a
+ * root was kept as 0, sqrt(v) in the parameter's next step is at least sqrt(beta2) times
+ * 2^-9 of the power it was kept with, the least root above 0 (divided by eps alone, m
+ * would make a step of hundreds of lr).  So 256 elements keep roots down to 2^-17 of
+ * their largest; smaller ones move by less than 32-bit states would have them.  With
+ * either kind of states the square of a gradient has to be within float32: below
+ * about 2^-70 v is 0, and eps alone is what m is divided by.
  */
 typedef enum { JANUS_ADAMW_F32 = 0, JANUS_ADAMW_8BIT = 1 } janus_adamw_states;
 

@@ -6,11 +6,14 @@ TEST INFRASTRUCTURE ONLY (see the package docstring).
     p <- p - lr decay p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 
 with s as in ``sgd``; nothing changes when the norm is not finite.  ``update`` is
-float64.  ``codes`` and ``moments32`` are the definition of the 8-bit states to the
+float64.  ``encode`` and ``moments32`` are the definition of the 8-bit states to the
 bit: each operation in float32 rounded by itself, the power of two of 256 elements,
-the random bits of an element and the rounding with them.
+the random bits of an element and the rounding with them.  ``least_root`` is what a
+root that 8 bits kept as 0 counts as at least in the next step of its parameter.
 """
 from __future__ import annotations
+
+import math
 
 import numpy as np
 
@@ -19,14 +22,16 @@ from . import sgd
 F = np.float32
 
 
-def update(p, g, m, v, step, lr, b1, b2, eps, decay, s):
-    """One tensor in float64: new p, m, v."""
+def update(p, g, m, v, step, lr, b1, b2, eps, decay, s, least=0.0):
+    """One tensor in float64: new p, m, v.  ``least``: sqrt(v) in the parameter's step
+    is this at least."""
     p, g, m, v = (np.asarray(a, np.float64) for a in (p, g, m, v))
     g = g * s
     m = b1 * m + (1.0 - b1) * g
     v = b2 * v + (1.0 - b2) * g * g
     t = step + 1
-    p = p - lr * decay * p - lr / (1.0 - b1 ** t) * m / (np.sqrt(v / (1.0 - b2 ** t)) + eps)
+    root = np.maximum(np.sqrt(v), least)
+    p = p - lr * decay * p - lr / (1.0 - b1 ** t) * m / (root / np.sqrt(1.0 - b2 ** t) + eps)
     return p, m, v
 
 
@@ -81,6 +86,13 @@ def decode(codes, scale):
     e, f = (c >> 3) & 15, c & 7
     v = np.where(e == 0, f * 2.0 ** -9, (8 + f) * 2.0 ** (e - 10.0)) * np.where(c & 128, -1.0, 1.0)
     return (v * np.repeat(np.asarray(scale, np.float64), 256)[:c.size]).astype(F)
+
+
+def least_root(codes, scale, b2):
+    """float64, for each element: sqrt(b2) times the least root above 0 that its block can
+    hold where the code of its own, before the step, is 0; else 0."""
+    c = np.asarray(codes)
+    return np.where(c == 0, math.sqrt(b2) * 2.0 ** -9 * np.repeat(np.asarray(scale, np.float64), 256)[:c.size], 0.0)
 
 
 def moments32(g, m, v, b1, b2, s):

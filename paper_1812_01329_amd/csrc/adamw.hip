@@ -17,7 +17,10 @@
 // at most 1.75 2^E, codes are e4m3 floats of x 2^(8 - E): exact but for the rounding
 // of the mantissa to 3 bits, which adds 16 random bits below them and cuts off.
 // sqrt(v) is kept in v's place: its range is half of v's in powers of two (e4m3
-// reaches 2^-18 of the largest), and half of v's relative step.
+// reaches 2^-18 of the largest), and half of v's relative step.  Where a root was kept as 0,
+// the parameter's step takes one of at least sqrt(b2) 2^-9 of its block's power, the least that
+// the block could have held: m has a power of its own and may be left, and m / eps is a step of
+// 470 lr half of a block's gradients of N(0, 1) after a single one of 1e-4 (so: 2.3).
 //
 // 19.8 M float32 parameters with 32-bit states: the norm 14.7 us (5.4 TB/s, partly from
 // the cache), the update 88 (6.3 TB/s with gradients in the cache; 108 us a call, where a
@@ -61,6 +64,7 @@ struct Control {
 struct AdamArgs {
     float b1, b2, c1, c2;        // c = 1 - b
     float eps, max_norm, lr;
+    float least;                 // sqrt(b2) 2^-9: a root of 0 in 8 bits in the next step, of its power of two
     uint32_t seed;
     int n_sums;
     double* sums;
@@ -196,7 +200,7 @@ __global__ __launch_bounds__(kThreads) void adamw_norm_kernel(Table t, AdamArgs 
 // One element: the moments and the parameter.  Every product and sum is rounded by
 // itself (contracted, the codes of 8 bits would depend on how the compiler paired them).
 struct Step {
-    float b1, b2, c1, c2, eps, s, rate, root, shrink;
+    float b1, b2, c1, c2, eps, s, rate, root, shrink, least;
     __device__ __forceinline__ void moments(float g, float& m, float& v) const {
 #pragma clang fp contract(off)
         g = g * s;
@@ -351,7 +355,7 @@ __device__ bool form_step(const AdamArgs& a, Step& st, Control& c, bool report) 
         if (go) *a.step = c.t;   // (the other workgroups have it from the control word)
     }
     st.b1 = a.b1, st.b2 = a.b2, st.c1 = a.c1, st.c2 = a.c2, st.eps = a.eps;
-    st.s = float(s), st.rate = c.rate, st.root = c.root, st.shrink = 0.f;
+    st.s = float(s), st.rate = c.rate, st.root = c.root, st.shrink = 0.f, st.least = a.least;
     return go;
 }
 
@@ -389,8 +393,10 @@ struct Four {
             decode(mc, scale.x, m);
             decode(vc, scale.y, v);
             uint32_t rm[4], rv[4];
+            float least[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                least[j] = v[j] == 0.f ? st.least * scale.y : 0.f;
                 v[j] = v[j] * v[j];
                 st.moments(g[j], m[j], v[j]);
                 r[j] = root_of(v[j]);
@@ -402,6 +408,8 @@ struct Four {
             store_codes<HOW>(static_cast<uint8_t*>(t.m) + e, k, cm);
             store_codes<HOW>(static_cast<uint8_t*>(t.v) + e, k, cv);
             if ((threadIdx.x & 63) == 0) *reinterpret_cast<float2*>(t.scale + e / 256 * 2) = s;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = r[j] < least[j] ? least[j] : r[j];   // (a NaN stays)
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -557,6 +565,7 @@ extern "C" janus_status janus_adamw_update(const janus_adamw_desc* d, const janu
     a.b1 = d->beta1, a.b2 = d->beta2;
     a.c1 = float(1.0 - double(d->beta1)), a.c2 = float(1.0 - double(d->beta2));
     a.eps = d->eps, a.max_norm = d->max_norm, a.lr = d->lr, a.seed = d->seed;
+    a.least = float(std::sqrt(double(d->beta2)) * 0x1p-9);
     a.step = step, a.lr_dev = lr, a.hold = hold, a.stats = stats;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool q = d->states == JANUS_ADAMW_8BIT;
