@@ -65,20 +65,23 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float* red) {
     }
 }
 
-// VEC elements at p.  ODD: wherever they start, and of the last ones only `left` are there (the
-// others are read as 0).
+// VEC elements at p.  ODD: wherever they start, and of the last ones only `left` (one at least) are
+// there; the others are read as 0, or with SAME as the first of them.
 template <typename T, int VEC, bool ODD>
 struct Span {
     Chan<T, VEC> c;
+    template <bool SAME = false>
     __device__ __forceinline__ void load(const T* p, int left) {
         if constexpr (!ODD) {
             c.load(p);
         } else if (left >= VEC) {
             __builtin_memcpy(&c.v, p, sizeof(c.v));
         } else if constexpr (sizeof(T) == 2) {
-            c.v = make_uint2(word(p, 0, left), word(p, 2, left));
+            const uint32_t none = SAME ? p[0] : 0;
+            c.v = make_uint2(word(p, 0, left, none), word(p, 2, left, none));
         } else {
-            c.v = make_float4(p[0], left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, 0.f);
+            const float none = SAME ? p[0] : 0.f;
+            c.v = make_float4(p[0], left > 1 ? p[1] : none, left > 2 ? p[2] : none, none);
         }
     }
     __device__ __forceinline__ void get(float* f) const { c.get(f); }
@@ -98,8 +101,8 @@ struct Span {
     }
 
   private:
-    __device__ __forceinline__ static uint32_t word(const T* p, int j, int left) {
-        return (j < left ? uint32_t(p[j]) : 0u) | (j + 1 < left ? uint32_t(p[j + 1]) << 16 : 0u);
+    __device__ __forceinline__ static uint32_t word(const T* p, int j, int left, uint32_t none) {
+        return (j < left ? uint32_t(p[j]) : none) | (j + 1 < left ? uint32_t(p[j + 1]) : none) << 16;
     }
 };
 template <int VEC, bool ODD>
@@ -226,7 +229,10 @@ __global__ __launch_bounds__(LANES > kThreads ? LANES : kThreads) void norm_fwd_
 
 // As the forward; a workgroup takes every gridDim.x-th group of rows.  65536 rows of 2048
 // bf16 take 215 us, a row in 256 threads; with a row in a wave, 32 elements a thread, 305
-// (registers leave too few waves).  P = 0: dx alone, by two reads of a row.
+// (registers leave too few waves).  P = 0: dx alone, by two reads of a row.  Past a row's end dy is
+// read as 0 and h as an element of the row: 0 may be further from the mean than float32
+// reaches, and 0 * inf would be in the row's sums (elements left out instead: registers
+// spilled, 14444 rows of 12001 bf16 4650 us instead of 481).
 constexpr int kBwdThreads = 512;   // (the fewer workgroups, the fewer sums of dgamma and dbeta)
 template <typename T, int VEC, bool ODD, int LANES, int P>
 __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void norm_bwd_kernel(NormArgs a) {
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void nor
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 const int c = (tid + i * LANES) * VEC;
-                if (c < a.D) hv[i].load(h + c, a.D - c), dv[i].load(dy + c, a.D - c);
+                if (c < a.D) hv[i].template load<true>(h + c, a.D - c), dv[i].load(dy + c, a.D - c);
             }
             float xh[P][VEC], g[P][VEC], s[2] = {0.f, 0.f};
 #pragma unroll
@@ -332,7 +338,7 @@ __global__ __launch_bounds__(LANES > kBwdThreads ? LANES : kBwdThreads) void nor
         auto load = [&](int64_t c) {
             Span<T, VEC, ODD> v;
             const int left = int(end - c);
-            v.load(h + c, left);
+            v.template load<true>(h + c, left);
             v.get(xh);
             v.load(dy + c, left);
             v.get(g);
