@@ -46,7 +46,8 @@ class SelectivePolicy:
 
     ``update`` = (lr, max_norm) appends the parameter update to the step (the
     float32 parameters of a bf16 model are updated by a call of their own, with
-    their own norm); an AdamW updates all of them in one call, under one norm."""
+    their own norm); an AdamW updates all of them in one call, under one norm, with
+    its decay on every matrix that its ``exempt`` does not name ("A" is one)."""
 
     def __init__(self, w: wl.PolicyWorkload, device="cuda", clip=(0.2, 0.2), kl_coef=0.0, ent_coef=0.0,
                  update: Union[Tuple[float, float], AdamW, None] = None):
@@ -82,7 +83,7 @@ class SelectivePolicy:
             self.dh = new(T * B, w.M)
         self.updates = []
         if isinstance(update, AdamW):
-            self.updates = [make_update(list(self.P.values()), [self.G[k] for k in self.P], update)]
+            self.updates = [make_update(list(self.P.values()), [self.G[k] for k in self.P], update, list(self.P))]
         elif update is not None:
             groups = [[k for k in self.P if self.P[k].dtype == dt] for dt in dict.fromkeys(p.dtype for p in self.P.values())]
             self.updates = [SgdUpdate([self.P[k] for k in g], [self.G[k] for k in g], *update) for g in groups]

@@ -59,9 +59,13 @@ class SgdUpdate:
 @dataclasses.dataclass
 class AdamW:
     """An ``update`` of the training steps in the place of (lr, max_norm):
-    AdamW with states of 32 or 8 bits.  ``decay`` is for the matrices (vectors,
-    biases and norms' scales among them, have none); ``masters`` keeps float32
-    copies of bf16 parameters."""
+    AdamW with states of 32 or 8 bits.  ``decay`` is for every parameter of two
+    dimensions (vectors, biases and norms' scales among them, have none) that
+    ``exempt`` does not name.  Parameters have the names of the step's attributes,
+    layers counted: "Wx[0]", "emb"; those of a policy the keys of its ``P``, where "A" (the
+    scan's decay rates, which a decay pulls towards states that never fade) and
+    "conv_w" (the convolution's taps) have two dimensions as well.  ``masters`` keeps
+    float32 copies of bf16 parameters."""
     lr: float
     max_norm: float = 0.0
     betas: Tuple[float, float] = (0.9, 0.999)
@@ -70,6 +74,7 @@ class AdamW:
     bits: int = 32
     masters: bool = False
     seed: int = 0
+    exempt: Tuple[str, ...] = ()
 
 
 class AdamWUpdate:
@@ -77,14 +82,21 @@ class AdamWUpdate:
     parameter tensor with its float32 gradient, float32 and bf16 parameters in one
     call under one norm.  Master copies are taken of the parameters as they are
     when the update is made (or from a state dict): parameters that are set later
-    need an update of their own."""
+    need an update of their own.  ``names`` are what the spec's ``exempt`` goes by."""
 
-    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], spec: AdamW):
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], spec: AdamW,
+                 names: Sequence[str] = ()):
         if spec.bits not in (8, 32):
             raise ValueError(f"states have 8 or 32 bits, not {spec.bits}")
         for p, g in zip(params, grads):
             if p.dtype not in (torch.float32, torch.bfloat16) or g.dtype != torch.float32 or p.numel() != g.numel():
                 raise ValueError("parameters are float32 or bf16, their gradients float32 of the same size")
+        exempt = (spec.exempt,) if isinstance(spec.exempt, str) else tuple(spec.exempt)
+        if set(exempt) - set(names):
+            raise ValueError(f"no parameter to exempt is named {sorted(set(exempt) - set(names))}; there are {list(names)}")
+        if names and len(names) != len(params):
+            raise ValueError(f"{len(names)} names for {len(params)} parameters")
+        bare = [names[i] in exempt if names else False for i in range(len(params))]
         q = spec.bits == 8
         dev, n = params[0].device, len(params)
         zeros = lambda p: torch.zeros(p.numel(), dtype=torch.uint8 if q else torch.float32, device=dev)
@@ -98,7 +110,7 @@ class AdamWUpdate:
         self.desc = J.AdamWDesc(n, J.ADAMW_8BIT if q else J.ADAMW_F32, spec.lr, *spec.betas, spec.eps, spec.max_norm,
                                 spec.seed)
         self.tensors = J.adamw_tensors(self.params, self.grads, self.m, self.v, self.scale, self.master,
-                                       [spec.decay if p.dim() > 1 else 0.0 for p in params])
+                                       [spec.decay if p.dim() > 1 and not b else 0.0 for p, b in zip(params, bare)])
         self.ws = torch.empty(J.janus_adamw_workspace_bytes(self.desc), dtype=torch.uint8, device=dev)
 
     def apply(self, hold: Optional[int] = None, lr: Optional[torch.Tensor] = None):
@@ -124,10 +136,10 @@ class AdamWUpdate:
                 t.copy_(new)
 
 
-def make_update(params, grads, update):
+def make_update(params, grads, update, names: Sequence[str] = ()):
     """The update of an ``update`` argument: (lr, max_norm) or an AdamW."""
     if isinstance(update, AdamW):
-        return AdamWUpdate(params, grads, update)
+        return AdamWUpdate(params, grads, update, names)
     return SgdUpdate(params, grads, *update)
 
 
@@ -205,7 +217,8 @@ class LSTMStep:
         self.update = None
         if update is not None:
             P, G = self.parameters()
-            self.update = make_update(P, G, update)
+            names = [f"{k}[{l}]" for l in range(w.L) for k in ("Wx", "Wh", "b")] + ["Wout", "bout", "E"]
+            self.update = make_update(P, G, update, names[:len(P)])
         # the timeout word of the step's recurrences: a step whose forward or
         # backward wait ran out leaves the parameters unchanged
         self.fault = J.janus_lstm_fault_flag(self.desc, self.ws)
@@ -311,7 +324,8 @@ class TreeStep:
         self.update = None
         if update is not None:
             self.update = make_update([self.emb, self.W, self.U, self.b, self.Ws, self.bs],
-                                      [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], update)
+                                      [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], update,
+                                      ("emb", "W", "U", "b", "Ws", "bs"))
 
     def run(self):
         w = self.w
@@ -363,7 +377,8 @@ class TreeRNNStep:
         self.update = None
         if update is not None:
             self.update = make_update([self.emb, self.W, self.b, self.Ws, self.bs],
-                                      [self.demb, self.dW, self.db, self.dWs, self.dbs], update)
+                                      [self.demb, self.dW, self.db, self.dWs, self.dbs], update,
+                                      ("emb", "W", "b", "Ws", "bs"))
 
     def run(self):
         w = self.w
@@ -416,7 +431,8 @@ class ChildSumStep:
         self.update = None
         if update is not None:
             self.update = make_update([self.emb, self.W, self.U, self.b, self.Ws, self.bs],
-                                      [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], update)
+                                      [self.demb, self.dW, self.dU, self.db, self.dWs, self.dbs], update,
+                                      ("emb", "W", "U", "b", "Ws", "bs"))
 
     def run(self):
         w = self.w
