@@ -154,6 +154,12 @@ struct Run {
 // bf16 take 11.4, 11.7 and 19.8 us in 256, 512 and 1024 threads, 2000 rows 24, 35 and 64;
 // 300 and 2000 rows of 16000 13.3 and 44 us in 512, 21.4 and 73 in 1024.
 constexpr int kHeld = 8192, kHeldSmall = 512, kHeldMiddle = 2048;
+// In a row that is not held, up to this many elements that min-p alone keeps are listed: marks are
+// met again in memory, by their weights and by the border.  Rows of 50257 float32 by list and by
+// marks: 20 rows that keep 12 14.7 and 20.3 us, 96 16.4 and 20.6, 200 21.1 and 20.9, 900 31.7 and 23.3;
+// 2000 rows 175, 188, 226 and 320 by list, 207, 211, 212 and 227 by marks (counting them is
+// 1 to 3 % on top).
+constexpr uint32_t kFewMarked = 128;
 template <int THREADS> constexpr int kSlots = THREADS == 256 ? 2 : THREADS == 512 ? 4 : 8;   // a thread's at most
 constexpr size_t held_bytes(int64_t np) { return size_t(np + 8) * 16; }  // (the last thread's pieces are turned as well)
 
@@ -747,8 +753,19 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, Sampler<T, THREA
     // With min-p alone nothing has to be ranked: the marked weights are added up where they are
     // (2000 rows of 1000 bf16 logits, min_p 0.05: 14.6 us, through a list 32.5; 2000 of 32768: 72 and 150).
     // A mark of two elements would be looked at again: the list is no slower then where it is short.
-    const bool marked = least > -INFINITY && some && k <= 0 && !part && s.few();
-    if (marked) add_marked(g.marks);
+    // Where the row is in memory a list is faster while it is short (kFewMarked).
+    bool marked = least > -INFINITY && some && k <= 0 && !part && s.few();
+    if (HELD) {
+        if (marked) add_marked(g.marks);
+    } else if (marked) {
+        const uint32_t c = last_lane(up_to(uint32_t(__popcll(g.marks))));
+        if (lane == 0 && c) atomicAdd(&sh.live, c);
+        const bool early = c * WAVES > kFewMarked;   // (a wave that has many does not wait to know)
+        if (early) add_marked(g.marks);
+        __syncthreads();
+        marked = sh.live > kFewMarked;
+        if (marked && !early) add_marked(g.marks);
+    }
     // sums of all, and of the threads before
     u64 all = 0, before = 0;
     if (sum_all) {
