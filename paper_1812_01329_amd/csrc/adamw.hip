@@ -24,8 +24,8 @@
 //
 // 19.8 M float32 parameters with 32-bit states: the norm 14.7 us (5.4 TB/s, partly from
 // the cache), the update 88 (6.3 TB/s with gradients in the cache; 108 us a call, where a
-// copy of the same bytes takes 117).  71 M of bf16 with masters and 8-bit states: 45 and 210 us
-// (255 a call, 273).  10 small tensors: 3.2 and 4.7 us, latency.
+// copy of the same bytes takes 117).  71 M of bf16 with masters and 8-bit states: 45 and 215 us
+// (257 a call, 273).  10 small tensors: 3.2 and 4.7 us, latency.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -8,7 +8,8 @@
 //
 // A row belongs to a group of 16 to 1024 threads, 8 elements a thread where that
 // suffices, and stays in registers from its mean to its result, so every tensor is
-// read and written once.  In the backward a thread has the same columns in every row it
+// read and written once (up to 16384 elements; float32 in the backward up to 8192: past
+// that registers spill, and a row is read again for every pass).  In the backward a thread has the same columns in every row it
 // meets and adds up their dgamma and dbeta; workgroups' sums go to the workspace, and a
 // second kernel adds them up in their order.  Everything between loads and stores is
 // float32; the variance is that of the differences from the mean (a mean of squares
@@ -478,8 +479,9 @@ NormArgs norm_args(const janus_norm_desc* d) {
 // Elements an aligned access: the most that rows' starts and ends allow.
 // Where that is fewer than four, the forward takes four wherever they start (ODD): 14444 rows of
 // 1409 bf16 27 us, by single elements 64; of 5946, by pairs, 144 and 165; of 1409 float32 34 and 37.
-// The backward does so for single bf16 alone (14444 of 12001: 490 and 935 us): its
-// pairs and its float32 elements are no slower by themselves (5946: 190 and 208 us; 268 and 299).
+// The backward does so for single bf16 alone (14444 rows of 12001: 484 us, by single elements 935).
+// Rows of 5946 bf16 take 188 us by pairs and 208 by four from anywhere, of 5946 float32 267 by
+// single elements (no multiple of four) and 299 by four from anywhere.
 int norm_vec(const NormArgs& a, size_t es, std::initializer_list<const void*> rows, std::initializer_list<int64_t> lds) {
     int vec = int(16 / es);
     for (; vec > 1; vec /= 2) {

@@ -25,10 +25,14 @@
 //         then among one thread's elements.  Min-p alone goes this way too.
 //
 // Few rows are bound by the chain of passes and scans between lanes: 20 rows of 10000 bf16
-// with top-k and top-p 9.6 us, 37 of 20001 float32 with min-p 11.1.  Many are bound by the
-// vector units where a sum of all is wanted (25 operations a weight, most in float64):
-// 1024 rows of 65536 bf16 take 85 us (1.6 TB/s), 91 with the weights of four elements in
-// turn; else by LDS: 2000 rows of 32768 bf16 with min-p 72 us (1.8 TB/s).  A row in
+// with top-k and top-p 9.6 us, 37 of 20001 float32 with min-p 11.1.  Many spend their time in the
+// vector units and in turns: a CU has room for one row past 16384 bf16, which it
+// loads, waits for at barriers and works on one after another.  1024 rows of 65536 bf16 with
+// nothing filtered take 85 us (1.6 TB/s): 32 vector instructions a logit, most of them a
+// weight's in float64, keep the units busy for 62 % of it (91 us with the weights of
+// four elements in turn).  2000 rows of 32768 bf16 with min-p take 72 us (1.8 TB/s; with the
+// log-probability the units are busy for 57 %, LDS for 6 %), 2000 of 40000 with top-p alone
+// 272: 96 instructions a logit, 76 %, and LDS with its atomics 16 %.  A row in
 // registers instead of LDS needs every pass unrolled, which the instruction cache does not
 // hold: 45 us for 37 rows where LDS took 20.
 #include <cmath>
