@@ -749,6 +749,9 @@ janus_status janus_policy_loss(const janus_policy_desc* d, const void* logits, c
  * Rows are independent: a row with an infinity or a NaN has NaN in its y and
  * dx, and in dgamma and dbeta.  Every row counts for those two; rows past a
  * sequence's end add nothing where their dy is 0 and their h finite.
+ * Sums are float32: a row whose squared differences from its mean add up to more than
+ * that holds (differences past about 1e19) has rstd 0 and, where its sum is finite, y =
+ * beta.
  */
 /* The ld* are the row strides, in elements, of x and dx (ldx), of r, h and dh
  * (ldh) and of y and dy (ldy); 0: dense, D; else at least D. */
